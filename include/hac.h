@@ -17,6 +17,10 @@
  *        number the values like the HAC alphabet: 0.0 first when it occurs,
  *        then ascending.
  *
+ *   MX   (an extension): entries of 4 bits, E2M1 floating point, with one power of two as
+ *        scale for every 32 consecutive rows of a column; for layers that are quantized without
+ *        a value list, and for the experts of a layer.  See mx_encode below.
+ *
  *   Network blobs (Sect. V-H, V-K): all layers of a network written with one
  *        shared dictionary, index-map layers sharing its value list; see
  *        hac_net_encode below.
@@ -74,7 +78,7 @@ typedef enum {
     HAC_EWORKSPACE = -6    /* workspace missing or smaller than hac_workspace_bytes()    */
 } hac_status;
 
-enum { HAC_FORMAT_HAC = 1, HAC_FORMAT_SHAC = 2, HAC_FORMAT_IM = 3 };
+enum { HAC_FORMAT_HAC = 1, HAC_FORMAT_SHAC = 2, HAC_FORMAT_IM = 3, HAC_FORMAT_MX = 4 };
 
 /* A hipStream_t, spelled without pulling in the HIP headers. */
 typedef void *hac_stream_t;
@@ -128,7 +132,7 @@ enum { HAC_RI_FIELDS = 0, HAC_RI_RICE = 1 };
 typedef struct {
     uint32_t magic;        /* 'HAC1' = 0x31434148                                          */
     uint32_t version;      /* 2                                                            */
-    uint32_t format;       /* HAC_FORMAT_HAC / HAC_FORMAT_SHAC                             */
+    uint32_t format;       /* HAC_FORMAT_*                                                 */
     uint32_t header_bytes; /* 256                                                          */
     uint64_t n, m;         /* shape of W                                                   */
     uint64_t nnz;          /* q: entries different from 0.0                                */
@@ -194,6 +198,12 @@ typedef struct {
  * the index map at off_stream, n rows of idx_pitch pointers, row-major (followed
  * by >= 64 bytes of zeros); total_bits = ent_bits * n * m, the paper's bbar*n*m;
  * has_zero as for HAC.  Every other offset and count is 0. */
+
+/* An MX blob holds k_sym matrices of n x m each (one layer, or the experts of one):
+ * format = HAC_FORMAT_MX; ent_bits = 4; chunk = 32, the entries of a block; total_bits
+ * = 4 * k_sym * n * m; the scales of all matrices at off_codebook, then the codes of all
+ * matrices at off_stream (their order: mx_encode below); nnz is not counted (0).
+ * Every other offset and count is 0, and the sizes determine the whole header. */
 
 /* Sizes as the paper accounts for them (Sect. IV-B/IV-C) next to the real ones. */
 typedef struct {
@@ -511,7 +521,7 @@ int hac_dot_noalloc(const hac_desc_t *desc, const void *d_blob,
 
 /* A chain of layers (not in the paper, which gives the product of one layer):
  *     A_0 = X,   A_{l+1} = act_l(A_l . W_l + bias_l),   Y = A_L
- * with W_l given compressed (HAC, sHAC or IM; layer blobs of their own or the
+ * with W_l given compressed (HAC, sHAC, IM or MX; layer blobs of their own or the
  * layers of a network blob), bias_l an optional vector of m_l floats added to
  * every row, act_l the identity or max(., 0).  Bias and activation are applied
  * where a sum is finished, and between two layers that both take the sparse
@@ -551,6 +561,71 @@ int im_dot(const hac_desc_t *desc, const void *d_blob,
            void *d_ws, size_t ws_bytes,
            const hac_launch_t *launch, hac_stream_t stream);
 
+/* ---- 4-bit microscaled layers (an extension) -------------------------------- */
+
+/* A block is 32 consecutive rows of a column (the last one of a column may be shorter).  With
+ * a = max |w| over the block its scale is 2^s, s = max(floor(log2 a) - 2, -127) (a = 0: -127),
+ * and an entry is +- one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 times the scale: the nearest, on ties the
+ * one with the even code, 6 for everything larger (codes 0 .. 7 in this order, + 8 for a negative
+ * entry, which -0.0 and what is rounded to it are too).
+ *
+ * Layout of one matrix, steps = ceil(n / 128), groups = ceil(steps / 4), tiles = ceil(m / 16):
+ *   codes : tiles x steps x 64 pieces of 16 bytes; piece 16 g + c of (t, s) holds the 32 codes of
+ *           rows 128 s + 32 g ... of column 16 t + c, the lower half of a byte first
+ *   scales: tiles x groups x 64 words of 4 bytes; byte b of word 16 g + c of (t, q) is s + 127 for
+ *           that column and the rows 512 q + 128 b + 32 g ...; 255 marks a block of NaN
+ * Codes and scales past row n or column m are 0.
+ *
+ * Values are X.W with W's entries so rounded: every value of W is exact in bfloat16 and sums are
+ * kept in fp32.  X and Y are fp32 or bfloat16 (type; Y is rounded once, to nearest); fp32 rows of
+ * X enter whole, as three bfloat16 parts, exactly but for what lies below 2^-133.  With
+ * HAC_MX_QUANTIZE_X the rows of X are quantised too, blocks of 32 entries of a row from its first
+ * on, in the same way as columns of W: the product is then that of two matrices of 4-bit entries.
+ * An infinity or NaN in X makes those results of its row NaN or infinite that the sum of its products
+ * makes so; with HAC_MX_QUANTIZE_X, all results of the row NaN. */
+enum { HAC_TYPE_F32 = 0, HAC_TYPE_BF16 = 1 };
+#define HAC_MX_QUANTIZE_X 0x1u
+
+/* The header of a blob of `count` matrices (1 .. 65535) of n x m: its size and where its sections
+ * lie.  Sizes no blob can have give HAC_EINVAL, more than 2^40 bytes of codes HAC_ERANGE. */
+int mx_describe(int64_t count, int64_t n, int64_t m, hac_desc_t *desc);
+
+/* Quantise and encode on the host: matrix e starts at W + e * stride (stride >= n * ldw when
+ * count > 1).  Ownership and errors as for hac_encode (NaN/Inf give HAC_EINVAL). */
+int mx_encode(const float *W, int64_t count, int64_t n, int64_t m, int64_t ldw, int64_t stride,
+              void **blob, size_t *blob_bytes);
+
+/* The same on the device, asynchronous on `stream`: d_blob (256-byte aligned) becomes byte for byte
+ * what mx_encode makes of the same values, header included; *desc receives the header.  A block with
+ * a NaN or infinity becomes 32 NaNs.  If d_blob is NULL or blob_capacity < desc->blob_bytes the call
+ * launches nothing and returns HAC_EWORKSPACE with desc filled in. */
+int mx_encode_dev(uint32_t type, const void *d_W, int64_t count, int64_t n, int64_t m, int64_t ldw, int64_t stride,
+                  void *d_blob, size_t blob_capacity, hac_desc_t *desc, hac_stream_t stream);
+
+/* The values of an MX blob, in fp32 or bfloat16 (exact in both), laid out as mx_encode's W. */
+int mx_decode_dev(const hac_desc_t *desc, const void *d_blob, uint32_t type, void *d_W, int64_t ldw, int64_t stride,
+                  hac_stream_t stream);
+
+/* Device workspace of mx_dot for B rows, or of mx_grouped_dot for B rows in all (grouped != 0); 0
+ * when none is needed and for arguments the calls refuse. */
+size_t mx_workspace_bytes(const hac_desc_t *desc, uint32_t type, int64_t B, uint32_t flags, int grouped);
+
+/* Y[B x m] = X[B x n] . W for a blob of one matrix.  Rows of X and Y may start at any element
+ * (ldx >= n, ldy >= m); Y must not overlap X.  d_ws 256-byte aligned.  Results are bitwise reproducible:
+ * sums are added in an order that the sizes alone determine. */
+int mx_dot(const hac_desc_t *desc, const void *d_blob, uint32_t type, const void *d_X, int64_t B, int64_t ldx,
+           void *d_Y, int64_t ldy, uint32_t flags, void *d_ws, size_t ws_bytes, hac_stream_t stream);
+
+/* The product of the rows of each group with the group's own matrix (a layer of experts, rows sorted
+ * by expert): row r of X with offsets[e] <= r < offsets[e + 1] is multiplied with matrix e.  d_offsets:
+ * k_sym + 1 int32 in device memory, read when the kernels run, ascending (equal ones: an empty group)
+ * and within 0 .. B.  Rows before offsets[0] and from offsets[k_sym] on are left as they are in Y.
+ * Offsets that do not ascend or lie outside 0 .. B leave the results undefined, never what lies outside
+ * X, Y and the workspace.  Otherwise as mx_dot. */
+int mx_grouped_dot(const hac_desc_t *desc, const void *d_blob, uint32_t type, const void *d_X, int64_t B, int64_t ldx,
+                   const int32_t *d_offsets, void *d_Y, int64_t ldy, uint32_t flags,
+                   void *d_ws, size_t ws_bytes, hac_stream_t stream);
+
 /* TEST ONLY: materialise what the device decoder sees.
  * d_W  : n*m floats, row-major (every entry written);
  * d_sym: n*m int32 symbols in column order (every entry written). */
@@ -563,7 +638,7 @@ int shac_decode_dev(const hac_desc_t *desc, const void *d_blob,
                     hac_stream_t stream);
 
 /* The kernels launched by the calling thread's most recent successful hac_dot / shac_dot /
- * im_dot / hac_dot_noalloc call, in launch order, separated by "; ", spelled as a profiler prints
+ * im_dot / hac_dot_noalloc or mx_ call, in launch order, separated by "; ", spelled as a profiler prints
  * them without their namespace (e.g. "transpose_panel32_kernel<128u>; dot_batch_kernel<false, 4, true,
  * false, 1>"), but for dot_split_kernel's last template argument, the kind of its sums.  For attributing profiler rows to calls; never NULL. */
 const char *hac_last_kernels(void);

@@ -20,6 +20,7 @@ _lib: Optional[C.CDLL] = None
 HAC_FORMAT_HAC = 1
 HAC_FORMAT_SHAC = 2
 HAC_FORMAT_IM = 3
+HAC_FORMAT_MX = 4
 
 EXPORTS = (
     "hac_encode", "shac_encode", "hac_free", "hac_validate", "hac_describe", "hac_stats",
@@ -28,6 +29,11 @@ EXPORTS = (
     "hac_encode_dev", "hac_encode_dev_alloc", "hac_encode_dev_workspace_bytes", "hac_choose_format",
     "hac_net_encode", "hac_net_describe", "hac_net_layer", "hac_net_validate", "hac_net_stats",
     "hac_net_decode_host", "hac_forward", "hac_forward_workspace_bytes", "hac_dot_noalloc", "hac_last_kernels",
+)
+
+# ... of the 4-bit microscaled layers
+MX_EXPORTS = (
+    "mx_describe", "mx_encode", "mx_encode_dev", "mx_decode_dev", "mx_workspace_bytes", "mx_dot", "mx_grouped_dot",
 )
 
 
@@ -170,7 +176,16 @@ def load_library() -> C.CDLL:
     lib.hac_last_hip_error.argtypes = []
     lib.hac_last_kernels.argtypes = []
     lib.hac_last_kernels.restype = C.c_char_p
-    for name in EXPORTS:
+    lib.mx_describe.argtypes = [C.c_int64, C.c_int64, C.c_int64, C.POINTER(Desc)]
+    lib.mx_encode.argtypes = [f32p] + 5 * [C.c_int64] + [C.POINTER(vp), C.POINTER(C.c_size_t)]
+    lib.mx_encode_dev.argtypes = [C.c_uint32, vp] + 5 * [C.c_int64] + [vp, C.c_size_t, C.POINTER(Desc), vp]
+    lib.mx_decode_dev.argtypes = [C.POINTER(Desc), vp, C.c_uint32, vp, C.c_int64, C.c_int64, vp]
+    lib.mx_workspace_bytes.argtypes = [C.POINTER(Desc), C.c_uint32, C.c_int64, C.c_uint32, C.c_int]
+    lib.mx_workspace_bytes.restype = C.c_size_t
+    lib.mx_dot.argtypes = [C.POINTER(Desc), vp, C.c_uint32, vp, C.c_int64, C.c_int64, vp, C.c_int64, C.c_uint32, vp, C.c_size_t, vp]
+    lib.mx_grouped_dot.argtypes = [C.POINTER(Desc), vp, C.c_uint32, vp, C.c_int64, C.c_int64, vp, vp, C.c_int64, C.c_uint32,
+                                   vp, C.c_size_t, vp]
+    for name in EXPORTS + MX_EXPORTS:
         getattr(lib, name)
     _lib = lib
     return lib
@@ -210,8 +225,15 @@ class Blob:
         """The library's sequential CPU decoder: (W, sym[, row, col])."""
         d = self.desc
         n, m, q = int(d.n), int(d.m), int(d.nnz)
-        W = np.empty((n, m), dtype=np.float32) if want_w else None
         f32p, i32p = C.POINTER(C.c_float), C.POINTER(C.c_int32)
+        if d.format == HAC_FORMAT_MX:
+            shape = (n, m) if d.k_sym == 1 else (int(d.k_sym), n, m)
+            W = np.empty(shape, dtype=np.float32) if want_w else None
+            sym = np.empty(int(d.k_sym) * n * m, dtype=np.int32)
+            _check(load_library().hac_decode_host(self.data.ctypes.data, self.data.size, W.ctypes.data_as(f32p) if want_w else None,
+                                                  sym.ctypes.data_as(i32p), None, None), "hac_decode_host")
+            return W, sym
+        W = np.empty((n, m), dtype=np.float32) if want_w else None
         wp = W.ctypes.data_as(f32p) if want_w else None
         if d.format in (HAC_FORMAT_HAC, HAC_FORMAT_IM):
             sym = np.empty(n * m, dtype=np.int32)
@@ -248,6 +270,11 @@ class DeviceBlob:
     @property
     def m(self) -> int:
         return int(self.desc.m)
+
+    @property
+    def count(self) -> int:
+        """Matrices in the blob: those of an MX blob, else 1."""
+        return int(self.desc.k_sym) if self.desc.format == HAC_FORMAT_MX else 1
 
 
 class NetBlob:
@@ -426,7 +453,8 @@ def _native():
         loader.exec_module(mod)
         lib = load_library()
         mod.bind(_check, Desc, Launch, *(C.cast(getattr(lib, f), C.c_void_p).value for f in (
-            "hac_dot", "shac_dot", "im_dot", "hac_dot_noalloc", "hac_workspace_bytes_for", "hac_forward", "hac_forward_workspace_bytes")))
+            "hac_dot", "shac_dot", "im_dot", "hac_dot_noalloc", "hac_workspace_bytes_for", "hac_forward", "hac_forward_workspace_bytes",
+            "mx_dot", "mx_grouped_dot", "mx_workspace_bytes", "mx_encode_dev", "mx_decode_dev", "mx_describe")))
         _bound = mod
     return _bound
 
@@ -509,6 +537,66 @@ def hac_dot_route(desc: Desc, B: int, launch: Optional["Launch"] = None) -> int:
 def im_dot(dblob: DeviceBlob, X, Y=None, workspace=None, stream=None):
     """Y = X . W for an index-map blob on the device (asynchronous on the stream)."""
     return (_bound or _native()).im_dot(dblob, X, Y, workspace, stream)
+
+
+TYPE_F32, TYPE_BF16 = 0, 1
+MX_QUANTIZE_X = 0x1
+
+
+def mx_describe(n: int, m: int, count: int = 1) -> Desc:
+    """The header of an MX blob of `count` matrices of n x m."""
+    desc = Desc()
+    _check(load_library().mx_describe(count, n, m, C.byref(desc)), "mx_describe")
+    return desc
+
+
+def mx_encode(W: np.ndarray) -> Blob:
+    """W (n x m float32, or count x n x m for the experts of a layer; host) -> MX blob: 4-bit entries, a scale per 32 rows."""
+    W = np.asarray(W)
+    if W.dtype != np.float32 or W.ndim not in (2, 3):
+        raise TypeError("W must be a 2-D or 3-D float32 array")
+    W = np.ascontiguousarray(W)
+    lib = load_library()
+    count, (n, m) = (W.shape[0] if W.ndim == 3 else 1), W.shape[-2:]
+    out, size = C.c_void_p(), C.c_size_t()
+    _check(lib.mx_encode(W.ctypes.data_as(C.POINTER(C.c_float)), count, n, m, m, n * m, C.byref(out), C.byref(size)), "mx_encode")
+    return Blob(_adopt(lib, out, size.value))
+
+
+def mx_encode_dev(W, stream=None) -> DeviceBlob:
+    """The same on the device: W is a 2-D or 3-D float32 or bfloat16 CUDA tensor (asynchronous on the stream)."""
+    desc = Desc()
+    return DeviceBlob(desc, (_bound or _native()).mx_encode_dev(desc, W, stream))
+
+
+def mx_decode_dev(dblob: DeviceBlob, dtype=None, W=None, stream=None):
+    """The values of an MX blob as float32 (default) or bfloat16, n x m, or count x n x m where there are several
+    (asynchronous on the stream); into W when it is given."""
+    return (_bound or _native()).mx_decode_dev(dblob, dtype, W, stream)
+
+
+def mx_workspace_bytes(desc: Desc, B: int, dtype=None, quantize: bool = False, grouped: bool = False) -> int:
+    """Workspace bytes of mx_dot, or of mx_grouped_dot, for B rows of float32 (default) or bfloat16."""
+    import torch
+    types = {None: TYPE_F32, torch.float32: TYPE_F32, torch.bfloat16: TYPE_BF16}
+    if dtype not in types:
+        raise TypeError("dtype must be float32 or bfloat16")
+    return int(load_library().mx_workspace_bytes(C.byref(desc), types[dtype], B, MX_QUANTIZE_X if quantize else 0, int(grouped)))
+
+
+def mx_dot(dblob: DeviceBlob, X, Y=None, workspace=None, quantize=False, stream=None):
+    """Y = X . W for an MX blob of one matrix; X float32 or bfloat16, Y of the same type (asynchronous on the stream).
+
+    quantize: the rows of X are rounded to 4-bit entries too, as columns of W are, before they are multiplied."""
+    return (_bound or _native()).mx_dot(dblob, X, Y, workspace, quantize, stream)
+
+
+def mx_grouped_dot(dblob: DeviceBlob, X, offsets, Y=None, workspace=None, quantize=False, stream=None):
+    """Rows offsets[e] .. offsets[e + 1] - 1 of X times matrix e of an MX blob (a layer of experts, rows sorted by expert).
+
+    offsets: count + 1 ascending int32 on the device.  Rows that belong to no expert are not written: they stay as they are in a
+    Y of the caller's, and are uninitialised in one made here."""
+    return (_bound or _native()).mx_grouped_dot(dblob, X, offsets, Y, workspace, quantize, stream)
 
 
 def _layer_array(layers):

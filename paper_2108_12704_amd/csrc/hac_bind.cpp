@@ -1,5 +1,5 @@
-// Native call path of the Python binding for the calls of a serving loop: hac_dot, shac_dot, im_dot, hac_dot_noalloc and
-// hac_forward on torch tensors.  Same checks, exceptions and results as the Python text they replace; nothing is kept
+// Native call path of the Python binding for the calls of a serving loop: hac_dot, shac_dot, im_dot, hac_dot_noalloc,
+// hac_forward and the device calls of 4-bit layers (mx_*) on torch tensors.  Same checks, exceptions and results as the Python text they replace; nothing is kept
 // between calls but the addresses of the library's functions.
 //
 // Why native: on small products the host, not the GPU, sets the time of a call.  A call through ctypes took 9 us of the
@@ -8,7 +8,9 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -27,6 +29,12 @@ struct Api {
     decltype(&::hac_workspace_bytes_for) ws_bytes;
     decltype(&::hac_forward) forward;
     decltype(&::hac_forward_workspace_bytes) forward_ws;
+    decltype(&::mx_dot) mx_dot;
+    decltype(&::mx_grouped_dot) mx_grouped;
+    decltype(&::mx_workspace_bytes) mx_ws;
+    decltype(&::mx_encode_dev) mx_encode;
+    decltype(&::mx_decode_dev) mx_decode;
+    decltype(&::mx_describe) mx_describe;
 } g_api;
 PyObject* g_error = nullptr;             // called with (status, function name): raises HacError
 PyObject *g_desc, *g_tensor, *g_stream;  // attribute names
@@ -338,12 +346,190 @@ PyObject* py_forward(PyObject*, PyObject* const* args, Py_ssize_t n, PyObject* k
     });
 }
 
-// bind(error, Desc, Launch, hac_dot, shac_dot, im_dot, hac_dot_noalloc, hac_workspace_bytes_for, hac_forward, hac_forward_workspace_bytes): addresses
+// ---- 4-bit layers: float32 or bfloat16, on the device of their tensors, whichever is current -----------------------------
+
+struct OnDevice {
+    c10::DeviceIndex before = -1;
+    explicit OnDevice(const at::Tensor& t)
+    {
+        const c10::DeviceIndex now = c10::hip::current_device(), want = t.device().index();
+        if (want != now) { c10::hip::set_device(want); before = now; }
+    }
+    ~OnDevice() { if (before >= 0) c10::hip::set_device(before); }
+    OnDevice(const OnDevice&) = delete;
+    OnDevice& operator=(const OnDevice&) = delete;
+};
+
+bool mx_typed(const at::Tensor& t) { return t.is_cuda() && (t.scalar_type() == at::kFloat || t.scalar_type() == at::kBFloat16); }
+uint32_t mx_type(const at::Tensor& t) { return t.scalar_type() == at::kFloat ? HAC_TYPE_F32 : HAC_TYPE_BF16; }
+
+void same_device(const at::Tensor& t, const at::Tensor& X, const char* what)
+{
+    if (t.device() != X.device()) raise(PyExc_ValueError, what);
+}
+
+// mx_dot(dblob, X, Y, workspace, quantize, stream) and mx_grouped_dot(dblob, X, offsets, Y, workspace, quantize, stream)
+PyObject* mx_product(bool grouped, PyObject* const* args, Py_ssize_t n, PyObject* kwnames)
+{
+    static const char* const names[] = { "dblob", "X", "Y", "workspace", "quantize", "stream" };
+    static const char* const grouped_names[] = { "dblob", "X", "offsets", "Y", "workspace", "quantize", "stream" };
+    return guarded([&]() -> PyObject* {
+        PyObject* a[7];                                      // as grouped_names
+        if (grouped) {
+            arguments(args, n, kwnames, grouped_names, 3, 7, a);
+        } else {
+            arguments(args, n, kwnames, names, 2, 6, a);
+            for (int i = 6; i > 2; --i) a[i] = a[i - 1];
+            a[2] = Py_None;
+        }
+        const char* what = "X must be a 2-D float32 or bfloat16 CUDA tensor";
+        at::Tensor X = tensor_of(a[1], what);
+        if (X.dim() != 2 || !mx_typed(X)) raise(PyExc_TypeError, what);
+        const OnDevice device(X);
+        const OnStream on(a[6], X);
+        X = with_rows(X);
+        const Blob blob(a[0]);
+        const hac_desc_t* d = blob.desc.get();
+        same_device(THPVariable_Unpack(blob.tensor_obj.p), X, "the blob and X must be on one device");
+        if (d->format != HAC_FORMAT_MX) raise(PyExc_ValueError, "the blob must be an MX blob");
+        const int64_t B = X.size(0), rows = (int64_t)d->n, m = (int64_t)d->m;
+        if (X.size(1) != rows) raise(PyExc_ValueError, "X has the wrong width");
+        const int32_t* offsets = nullptr;
+        if (grouped) {
+            what = "offsets must be a contiguous int32 CUDA tensor of count + 1 elements";
+            const at::Tensor& o = tensor_of(a[2], what);
+            if (o.scalar_type() != at::kInt || !o.is_cuda() || o.dim() != 1 || (uint64_t)o.numel() != (uint64_t)d->k_sym + 1 || !o.is_contiguous())
+                raise(PyExc_TypeError, what);
+            same_device(o, X, "offsets and X must be on one device");
+            offsets = static_cast<const int32_t*>(o.data_ptr());
+        }
+        const int quantize = a[5] == Py_None ? 0 : PyObject_IsTrue(a[5]);
+        if (quantize < 0) throw Raised{};
+        const uint32_t type = mx_type(X), flags = quantize ? HAC_MX_QUANTIZE_X : 0u;
+        at::Tensor Y;
+        if (a[3] == Py_None) {
+            Y = empty({B, m}, X.scalar_type(), X);
+            on.hand_over(Y);
+        } else {
+            what = "Y must be a B x m CUDA tensor of X's type with unit column stride";
+            Y = tensor_of(a[3], what);
+            if (Y.scalar_type() != X.scalar_type() || !Y.is_cuda() || Y.dim() != 2 || Y.size(0) != B || Y.size(1) != m || (m > 1 && Y.stride(1) != 1))
+                raise(PyExc_TypeError, what);
+            same_device(Y, X, "Y and X must be on one device");
+        }
+        const Scratch ws = scratch(a[4], X, a[4] == Py_None ? g_api.mx_ws(d, type, B, flags, grouped) : 0);
+        if (ws.keep.defined()) same_device(ws.keep, X, "the workspace and X must be on one device");
+        const int64_t ldx = B > 1 ? X.stride(0) : std::max<int64_t>(rows, 1), ldy = B > 1 ? Y.stride(0) : std::max<int64_t>(m, 1);
+        const void* x = X.data_ptr();
+        void* y = Y.data_ptr();
+        int rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = grouped ? g_api.mx_grouped(d, blob.data, type, x, B, ldx, offsets, y, ldy, flags, ws.ptr, ws.bytes, on.handle)
+                     : g_api.mx_dot(d, blob.data, type, x, B, ldx, y, ldy, flags, ws.ptr, ws.bytes, on.handle);
+        Py_END_ALLOW_THREADS
+        check(rc, grouped ? "mx_grouped_dot" : "mx_dot");
+        if (a[3] != Py_None) { Py_INCREF(a[3]); return a[3]; }
+        return THPVariable_Wrap(std::move(Y));
+    });
+}
+
+PyObject* py_mx_dot(PyObject*, PyObject* const* args, Py_ssize_t n, PyObject* kw) { return mx_product(false, args, n, kw); }
+PyObject* py_mx_grouped(PyObject*, PyObject* const* args, Py_ssize_t n, PyObject* kw) { return mx_product(true, args, n, kw); }
+
+// where the matrices of W lie: ldw, and the distance from one to the next
+void mx_strides(const at::Tensor& W, int64_t* ldw, int64_t* stride)
+{
+    const int64_t r = W.dim() - 2, rows = W.size(r), m = W.size(r + 1);
+    *ldw = rows > 1 ? W.stride(r) : std::max<int64_t>(m, 1);
+    *stride = r && W.size(0) > 1 ? W.stride(0) : rows * *ldw;
+}
+
+// mx_encode_dev(desc, W, stream) -> the blob's bytes; desc receives the header
+PyObject* py_mx_encode(PyObject*, PyObject* const* args, Py_ssize_t n, PyObject* kwnames)
+{
+    static const char* const names[] = { "desc", "W", "stream" };
+    return guarded([&]() -> PyObject* {
+        PyObject* a[3];
+        arguments(args, n, kwnames, names, 2, 3, a);
+        const char* what = "W must be a 2-D or 3-D float32 or bfloat16 CUDA tensor with unit column stride";
+        const at::Tensor& W = tensor_of(a[1], what);
+        if ((W.dim() != 2 && W.dim() != 3) || !mx_typed(W) || (W.size(-1) > 1 && W.stride(-1) != 1)) raise(PyExc_TypeError, what);
+        const OnDevice device(W);
+        const OnStream on(a[2], W);
+        const Struct<hac_desc_t> desc(a[0], g_Desc);
+        hac_desc_t* d = const_cast<hac_desc_t*>(desc.get());  // (of the caller's own, made for this call)
+        const int64_t count = W.dim() == 3 ? W.size(0) : 1, rows = W.size(-2), m = W.size(-1);
+        check(g_api.mx_describe(count, rows, m, d), "mx_encode_dev");
+        int64_t ldw, stride;
+        mx_strides(W, &ldw, &stride);
+        at::Tensor blob = empty({(int64_t)d->blob_bytes}, at::kByte, W);
+        on.hand_over(blob);
+        const void* w = W.data_ptr();
+        void* to = blob.data_ptr();
+        const size_t room = (size_t)d->blob_bytes;
+        int rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = g_api.mx_encode(mx_type(W), w, count, rows, m, ldw, stride, to, room, d, on.handle);
+        Py_END_ALLOW_THREADS
+        check(rc, "mx_encode_dev");
+        return THPVariable_Wrap(std::move(blob));
+    });
+}
+
+// mx_decode_dev(dblob, dtype, W, stream)
+PyObject* py_mx_decode(PyObject*, PyObject* const* args, Py_ssize_t n, PyObject* kwnames)
+{
+    static const char* const names[] = { "dblob", "dtype", "W", "stream" };
+    return guarded([&]() -> PyObject* {
+        PyObject* a[4];
+        arguments(args, n, kwnames, names, 1, 4, a);
+        const Blob blob(a[0]);
+        const hac_desc_t* d = blob.desc.get();
+        const at::Tensor& bytes = THPVariable_Unpack(blob.tensor_obj.p);
+        if (!bytes.is_cuda()) raise(PyExc_TypeError, "the blob must be in device memory");
+        if (d->format != HAC_FORMAT_MX) raise(PyExc_ValueError, "the blob must be an MX blob");
+        at::ScalarType type = at::kFloat;
+        if (a[1] != Py_None) {
+            if (!THPDtype_Check(a[1])) raise(PyExc_TypeError, "dtype must be float32 or bfloat16");
+            type = reinterpret_cast<THPDtype*>(a[1])->scalar_type;
+            if (type != at::kFloat && type != at::kBFloat16) raise(PyExc_TypeError, "dtype must be float32 or bfloat16");
+        }
+        const OnDevice device(bytes);
+        const OnStream on(a[3], bytes);
+        std::vector<int64_t> shape{(int64_t)d->n, (int64_t)d->m};
+        if (d->k_sym > 1) shape.insert(shape.begin(), (int64_t)d->k_sym);
+        at::Tensor W;
+        if (a[2] == Py_None) {
+            W = empty(shape, type, bytes);
+            on.hand_over(W);
+        } else {
+            const char* what = "W must be an n x m (count x n x m) CUDA tensor of the asked type with unit column stride";
+            W = tensor_of(a[2], what);
+            if (!mx_typed(W) || (a[1] != Py_None && W.scalar_type() != type) || W.sizes() != at::IntArrayRef(shape) || (W.size(-1) > 1 && W.stride(-1) != 1))
+                raise(PyExc_TypeError, what);
+            same_device(W, bytes, "W and the blob must be on one device");
+        }
+        int64_t ldw, stride;
+        mx_strides(W, &ldw, &stride);
+        void* to = W.data_ptr();
+        int rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = g_api.mx_decode(d, blob.data, mx_type(W), to, ldw, stride, on.handle);
+        Py_END_ALLOW_THREADS
+        check(rc, "mx_decode_dev");
+        if (a[2] != Py_None) { Py_INCREF(a[2]); return a[2]; }
+        return THPVariable_Wrap(std::move(W));
+    });
+}
+
+// bind(error, Desc, Launch, hac_dot, shac_dot, im_dot, hac_dot_noalloc, hac_workspace_bytes_for, hac_forward, hac_forward_workspace_bytes,
+// mx_dot, mx_grouped_dot, mx_workspace_bytes, mx_encode_dev, mx_decode_dev, mx_describe): addresses
 PyObject* py_bind(PyObject*, PyObject* args)
 {
     PyObject *error, *desc, *launch;
-    unsigned long long p[7];
-    if (!PyArg_ParseTuple(args, "OO!O!KKKKKKK", &error, &PyType_Type, &desc, &PyType_Type, &launch, p, p + 1, p + 2, p + 3, p + 4, p + 5, p + 6)) return nullptr;
+    unsigned long long p[13];
+    if (!PyArg_ParseTuple(args, "OO!O!KKKKKKKKKKKKK", &error, &PyType_Type, &desc, &PyType_Type, &launch, p, p + 1, p + 2, p + 3, p + 4, p + 5, p + 6,
+                          p + 7, p + 8, p + 9, p + 10, p + 11, p + 12)) return nullptr;
     Py_INCREF(error); Py_INCREF(desc); Py_INCREF(launch);
     Py_XDECREF(g_error); Py_XDECREF(g_Desc); Py_XDECREF(g_Launch);
     g_error = error; g_Desc = desc; g_Launch = launch;
@@ -354,6 +540,12 @@ PyObject* py_bind(PyObject*, PyObject* args)
     g_api.ws_bytes = reinterpret_cast<decltype(g_api.ws_bytes)>(p[4]);
     g_api.forward = reinterpret_cast<decltype(g_api.forward)>(p[5]);
     g_api.forward_ws = reinterpret_cast<decltype(g_api.forward_ws)>(p[6]);
+    g_api.mx_dot = reinterpret_cast<decltype(g_api.mx_dot)>(p[7]);
+    g_api.mx_grouped = reinterpret_cast<decltype(g_api.mx_grouped)>(p[8]);
+    g_api.mx_ws = reinterpret_cast<decltype(g_api.mx_ws)>(p[9]);
+    g_api.mx_encode = reinterpret_cast<decltype(g_api.mx_encode)>(p[10]);
+    g_api.mx_decode = reinterpret_cast<decltype(g_api.mx_decode)>(p[11]);
+    g_api.mx_describe = reinterpret_cast<decltype(g_api.mx_describe)>(p[12]);
     Py_RETURN_NONE;
 }
 
@@ -361,6 +553,8 @@ PyObject* py_bind(PyObject*, PyObject* args)
 PyMethodDef methods[] = {
     HAC_FAST("hac_dot", py_hac_dot), HAC_FAST("shac_dot", py_shac_dot), HAC_FAST("im_dot", py_im_dot),
     HAC_FAST("hac_dot_noalloc", py_noalloc), HAC_FAST("hac_forward", py_forward),
+    HAC_FAST("mx_dot", py_mx_dot), HAC_FAST("mx_grouped_dot", py_mx_grouped), HAC_FAST("mx_encode_dev", py_mx_encode),
+    HAC_FAST("mx_decode_dev", py_mx_decode),
     { "bind", py_bind, METH_VARARGS, nullptr }, { nullptr, nullptr, 0, nullptr } };
 PyModuleDef module = { PyModuleDef_HEAD_INIT, "_hacbind", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr };
 

@@ -4,6 +4,7 @@
 // the GPU (the paper's conclusions only suggest per-column offsets).
 #include "../../include/hac.h"
 #include "hac_hostlib.h"
+#include "hac_mx.h"
 
 #include <algorithm>
 #include <array>
@@ -12,6 +13,7 @@
 #include <cstdlib>
 #include <cstring>
 #include <functional>
+#include <limits>
 #include <memory>
 #include <new>
 #include <queue>
@@ -1198,6 +1200,123 @@ extern "C" int im_encode(const float* W, int64_t n, int64_t m, int64_t ldw,
     }
 }
 
+// ---- 4-bit microscaled blobs ------------------------------------------------------
+namespace {
+
+const float kMxValues[8] = { 0.0f, 0.5f, 1.0f, 1.5f, 2.0f, 3.0f, 4.0f, 6.0f };
+
+// code of v under the scale of byte `sb`; in 64 bits, where v / scale is exact
+uint32_t mx_code(float v, uint32_t sb)
+{
+    static const double border[7] = { 0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0 };
+    const double a = std::ldexp(std::fabs((double)v), 127 - (int)sb);
+    uint32_t c = 0;
+    for (int i = 0; i < 7; ++i) c += (i & 1) ? a >= border[i] : a > border[i];   // a border goes to the even code
+    return c | (std::signbit(v) ? 8u : 0u);
+}
+
+float mx_value(uint32_t code, uint32_t sb)
+{
+    if (sb == 255) return std::numeric_limits<float>::quiet_NaN();
+    const float v = (float)std::ldexp((double)kMxValues[code & 7], (int)sb - 127);
+    return code & 8 ? -v : v;
+}
+
+// deep: scales that an encoder writes, zeros past n and m
+int check_mx(const void* blob, const hac_desc_t& d, bool deep)
+{
+    if (!deep) return HAC_OK;
+    const uint8_t* base = static_cast<const uint8_t*>(blob);
+    const MxShape s = mx_shape(d.n, d.m);
+    for (uint64_t e = 0; e < d.k_sym; ++e) {
+        const uint8_t* scales = base + d.off_codebook + e * s.scale_bytes;
+        const uint8_t* codes = base + d.off_stream + e * s.code_bytes;
+        for (uint64_t j = 0; j < s.ctiles * kMxTileCols; ++j)
+            for (uint64_t b = 0; b < s.groups * 16; ++b) {
+                const bool inside = j < d.m && b * kMxBlock < d.n;
+                const uint8_t sb = scales[mx_scale_at(s, b, j)];
+                if (inside ? (sb > 252 && sb != 255) : sb != 0) return HAC_EFORMAT;
+                if (b >= s.steps * 4) continue;
+                const uint8_t* c = codes + mx_code_at(s, b, j);
+                for (uint64_t i = 0; i < kMxBlock; ++i)
+                    if ((!inside || b * kMxBlock + i >= d.n) && (c[i / 2] >> (i % 2 * 4) & 15)) return HAC_EFORMAT;
+            }
+    }
+    return HAC_OK;
+}
+
+int decode_mx(const void* blob, const hac_desc_t& d, float* W_out, int32_t* sym_out)
+{
+    const uint8_t* base = static_cast<const uint8_t*>(blob);
+    const MxShape s = mx_shape(d.n, d.m);
+    for (uint64_t e = 0; e < d.k_sym; ++e) {
+        const uint8_t* scales = base + d.off_codebook + e * s.scale_bytes;
+        const uint8_t* codes = base + d.off_stream + e * s.code_bytes;
+        for (uint64_t j = 0; j < d.m; ++j)
+            for (uint64_t i = 0; i < d.n; ++i) {
+                const uint64_t b = i / kMxBlock;
+                const uint32_t c = codes[mx_code_at(s, b, j) + i % kMxBlock / 2] >> (i % 2 * 4) & 15;
+                if (sym_out) sym_out[e * d.n * d.m + j * d.n + i] = (int32_t)c;
+                if (W_out) W_out[e * d.n * d.m + i * d.m + j] = mx_value(c, scales[mx_scale_at(s, b, j)]);
+            }
+    }
+    return HAC_OK;
+}
+
+} // namespace
+
+extern "C" int mx_describe(int64_t count, int64_t n, int64_t m, hac_desc_t* desc)
+{
+    if (!desc || count < 1 || count > (int64_t)kMxMaxCount || n < 1 || m < 1 || n > 0x7fffff00ll || m > 0x7fffff00ll) return HAC_EINVAL;
+    return mx_header(count, n, m, *desc) ? HAC_OK : HAC_ERANGE;
+}
+
+extern "C" int mx_encode(const float* W, int64_t count, int64_t n, int64_t m, int64_t ldw, int64_t stride,
+                         void** blob, size_t* blob_bytes)
+{
+    int rc = check_args(W, n, m, ldw, blob, blob_bytes);
+    if (rc) return rc;
+    *blob = nullptr; *blob_bytes = 0;
+    hac_desc_t d;
+    if ((rc = mx_describe(count, n, m, &d))) return rc;
+    if (count > 1 && (stride < 0 || stride / ldw < n)) return HAC_EINVAL;
+    try {
+        std::unique_ptr<void, void (*)(void*)> room(std::calloc(1, (size_t)d.blob_bytes), std::free);
+        uint8_t* base = static_cast<uint8_t*>(room.get());
+        if (!base) return HAC_ENOMEM;
+        std::memcpy(base, &d, sizeof d);
+        const MxShape s = mx_shape(d.n, d.m);
+        const uint64_t blocks = (d.n + kMxBlock - 1) / kMxBlock, items = (uint64_t)count * blocks;
+        std::atomic<bool> bad{false};
+        Team team((uint64_t)count * d.n * d.m, kGrain);
+        const uint64_t parts = std::min<uint64_t>(items, 64);
+        team.run(parts, [&](uint64_t t) {
+            std::vector<uint32_t> most((size_t)d.m);
+            for (uint64_t it = t * items / parts; it < (t + 1) * items / parts; ++it) {
+                const uint64_t e = it / blocks, b = it % blocks, rows = std::min<uint64_t>(kMxBlock, d.n - b * kMxBlock);
+                const float* w = W + (int64_t)e * (count > 1 ? stride : 0) + (int64_t)(b * kMxBlock) * ldw;
+                uint8_t* scales = base + d.off_codebook + e * s.scale_bytes;
+                uint8_t* codes = base + d.off_stream + e * s.code_bytes;
+                std::fill(most.begin(), most.end(), 0u);
+                for (uint64_t i = 0; i < rows; ++i)
+                    for (uint64_t j = 0; j < d.m; ++j) most[(size_t)j] = std::max(most[(size_t)j], float_bits(w[(int64_t)i * ldw + (int64_t)j]) & 0x7fffffffu);
+                for (uint64_t j = 0; j < d.m; ++j) {
+                    if (most[(size_t)j] >= 0x7f800000u) { bad = true; return; }
+                    scales[mx_scale_at(s, b, j)] = (uint8_t)mx_scale_byte(most[(size_t)j]);
+                }
+                for (uint64_t i = 0; i < rows; ++i)
+                    for (uint64_t j = 0; j < d.m; ++j)
+                        codes[mx_code_at(s, b, j) + i / 2] |= (uint8_t)(mx_code(w[(int64_t)i * ldw + (int64_t)j], mx_scale_byte(most[(size_t)j])) << (i % 2 * 4));
+            }
+        });
+        if (bad) return HAC_EINVAL;
+        *blob = room.release(); *blob_bytes = (size_t)d.blob_bytes;
+        return HAC_OK;
+    } catch (const std::bad_alloc&) {
+        return HAC_ENOMEM;
+    }
+}
+
 extern "C" void hac_free(void* blob) { std::free(blob); }
 
 // =================================================================================
@@ -1219,6 +1338,7 @@ int check_desc(const hac_desc_t& d, size_t bytes, bool in_net)
     if (d.magic != kMagic || d.version != kVersion || d.header_bytes != 256) return HAC_EFORMAT;
     if (d.dict_shared != (in_net ? 1u : 0u)) return HAC_EFORMAT;
 
+    if (d.format == HAC_FORMAT_MX) return !in_net && mx_header_ok(d) && d.blob_bytes <= bytes ? HAC_OK : HAC_EFORMAT;
     if (d.format != HAC_FORMAT_HAC && d.format != HAC_FORMAT_SHAC && d.format != HAC_FORMAT_IM) return HAC_EFORMAT;
     if (d.blob_bytes > bytes || d.blob_bytes < sizeof(hac_desc_t)) return HAC_EFORMAT;
     if (d.n < 1 || d.m < 1 || d.n > 0x7fffffffull || d.m > 0x7fffffffull) return HAC_EFORMAT;
@@ -1646,6 +1766,7 @@ extern "C" int hac_validate(const void* blob, size_t bytes, int deep)
     int rc = check_header(blob, bytes, d);
     if (rc) return rc;
     if (d.format == HAC_FORMAT_IM) return check_index_map(blob, d, deep != 0);
+    if (d.format == HAC_FORMAT_MX) return check_mx(blob, d, deep != 0);
     try {
         View v; make_view(blob, d, v);
         if ((rc = check_tables(v))) return rc;
@@ -1773,6 +1894,31 @@ extern "C" int hac_stats(const void* blob, size_t bytes, hac_stats_t* out)
         out->psi = (double)d.blob_bytes / (4.0 * nm);
         return HAC_OK;
     }
+    if (d.format == HAC_FORMAT_MX) {                               // scales counted as the tables, one byte per 32 entries in paper_bits
+        if ((rc = check_mx(blob, d, true))) return rc;
+        std::memset(out, 0, sizeof *out);
+        const MxShape s = mx_shape(d.n, d.m);
+        const double entries = (double)d.k_sym * (double)d.n * (double)d.m;
+        out->stream_bits = d.total_bits;
+        out->stream_bytes = d.k_sym * s.code_bytes;
+        out->table_bytes = d.k_sym * s.scale_bytes;
+        out->blob_bytes = d.blob_bytes;
+        out->paper_bits = d.total_bits + 8ull * d.k_sym * ((d.n + kMxBlock - 1) / kMxBlock) * d.m;
+        out->bound_bits = (double)out->paper_bits;
+        const uint8_t* base = static_cast<const uint8_t*>(blob);
+        uint64_t cnt[16] = {};
+        for (uint64_t e = 0; e < d.k_sym; ++e)
+            for (uint64_t j = 0; j < d.m; ++j)
+                for (uint64_t i = 0; i < d.n; ++i)
+                    cnt[base[d.off_stream + e * s.code_bytes + mx_code_at(s, i / kMxBlock, j) + i % kMxBlock / 2] >> (i % 2 * 4) & 15]++;
+        double H = 0.0;
+        for (uint64_t c : cnt)
+            if (c) { const double p = (double)c / entries; H -= p * std::log2(p); }
+        out->entropy_bits = H;
+        out->avg_code_bits = 4.0;
+        out->psi = (double)d.blob_bytes / (4.0 * entries);
+        return HAC_OK;
+    }
     View v; make_view(blob, d, v);
     if ((rc = check_tables(v))) return rc;
     if ((rc = check_index_shallow(v))) return rc;
@@ -1820,6 +1966,10 @@ extern "C" int hac_decode_host(const void* blob, size_t bytes, float* W_out, int
         if (row_out || col_out) return HAC_EINVAL;
         if ((rc = check_index_map(blob, d, true))) return rc;
         return decode_index_map(blob, d, W_out, sym_out);
+    }
+    if (d.format == HAC_FORMAT_MX) {
+        if (row_out || col_out) return HAC_EINVAL;
+        return decode_mx(blob, d, W_out, sym_out);
     }
     View v; make_view(blob, d, v);
     if ((rc = check_tables(v))) return rc;

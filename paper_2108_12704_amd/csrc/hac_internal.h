@@ -6,6 +6,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include "../../include/hac.h"
+
 namespace hac_internal {
 
 // How launch_index_gemm splits the work: `tiles` output tiles, each K loop of `steps` steps cut into
@@ -28,6 +30,11 @@ GemmPlan plan_index_gemm(uint32_t B, uint32_t n, uint32_t m, size_t room = ~(siz
 hipError_t launch_index_gemm(const GemmPlan& plan, const float* d_X, uint64_t ldx, uint32_t B, const void* d_idx, uint32_t idx_bits,
                              uint64_t pitch, const float* d_codebook, uint32_t k_sym, uint32_t zero_first,
                              uint32_t n, uint32_t m, float* d_Y, uint64_t ldy, float* d_part, hipStream_t stream);
+
+// An MX layer of a chain: mx_dot on fp32 rows and the workspace it takes, launches noted behind those that are noted already.
+size_t mx_layer_bytes(const hac_desc_t* desc, int64_t B);
+int mx_layer(const hac_desc_t* desc, const void* d_blob, const float* d_X, int64_t B, int64_t ldx, float* d_Y, int64_t ldy,
+             void* d_ws, size_t ws_bytes, hac_stream_t stream);
 
 // The kernels the calling thread's most recent dot call launched, by the names a profiler shows
 // (see hac_last_kernels): note_reset() at the start of a call, note_kernel() at every launch.

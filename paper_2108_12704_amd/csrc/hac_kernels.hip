@@ -30,6 +30,7 @@
 #include "../../include/hac.h"
 #include "hac_internal.h"
 #include "hac_hostlib.h"
+#include "hac_mx.h"
 #include "hac_device.h"
 
 // Optional phase timing (build with -DHAC_PHASE_TIMING): lane 0 of each wave of the dot
@@ -956,6 +957,8 @@ int hip_fail(hipError_t e) { g_last_hip_error = (int)e; return HAC_EHIP; }
 
 // What the planning calls need of a header before they divide by its fields (the device calls
 // check more, in make_dev and im_dot_impl).
+bool is_mx(const hac_desc_t* d) { return d && d->format == HAC_FORMAT_MX; }
+
 bool desc_plausible(const hac_desc_t* d)
 {
     if (!d || d->magic != 0x31434148u || d->version != 2) return false;
@@ -1801,6 +1804,7 @@ size_t workspace_need(const hac_desc_t* desc, int64_t B, const hac_launch_t* lau
 
 extern "C" size_t hac_workspace_bytes_for(const hac_desc_t* desc, int64_t B, const hac_launch_t* launch)
 {
+    if (is_mx(desc)) return hac_internal::mx_layer_bytes(desc, B);
     if (!desc_plausible(desc) || B <= 0 || B > 0x7fffffffll) return 0;
     if (desc->format == HAC_FORMAT_IM)
         return hac_internal::plan_index_gemm((uint32_t)B, (uint32_t)desc->n, (uint32_t)desc->m).part_bytes;
@@ -1861,7 +1865,7 @@ constexpr uint32_t kMaxChain = 256;
 
 bool layer_sparse(const hac_desc_t* desc, int64_t B)
 {
-    return desc->format != HAC_FORMAT_IM && !dense_route(desc, B, nullptr).use;
+    return desc->format != HAC_FORMAT_IM && desc->format != HAC_FORMAT_MX && !dense_route(desc, B, nullptr).use;
 }
 
 int plan_chain(const hac_layer_t* layers, uint32_t L, int64_t B, ChainPlan& P)
@@ -1873,16 +1877,23 @@ int plan_chain(const hac_layer_t* layers, uint32_t L, int64_t B, ChainPlan& P)
         const hac_desc_t* d = layers[l].desc;
         if (!d || !layers[l].d_blob || layers[l].activation > HAC_ACT_RELU || layers[l].reserved) return HAC_EINVAL;
         if (d->magic != 0x31434148u || d->version != 2) return HAC_EINVAL;
-        if (d->format != HAC_FORMAT_HAC && d->format != HAC_FORMAT_SHAC && d->format != HAC_FORMAT_IM) return HAC_EINVAL;
-        if (!desc_plausible(d)) return HAC_EINVAL;
+        if (is_mx(d)) {
+            if (!hac_internal::mx_header_ok(*d) || d->k_sym != 1) return HAC_EINVAL;
+        } else {
+            if (d->format != HAC_FORMAT_HAC && d->format != HAC_FORMAT_SHAC && d->format != HAC_FORMAT_IM) return HAC_EINVAL;
+            if (!desc_plausible(d)) return HAC_EINVAL;
+        }
         if (l && d->n != layers[l - 1].desc->m) return HAC_EINVAL;
     }
     if (!B) return HAC_OK;
     for (uint32_t l = 0; l < L; ++l) {
         const hac_desc_t* d = layers[l].desc;
         P.sparse[l] = layer_sparse(d, B);
-        const SplitPlan sp = plan_split(d, B, nullptr);
-        P.wants_xt[l] = P.sparse[l] && (sp.use ? !sp.direct : !xlds_plan(d, B, nullptr).use);
+        P.wants_xt[l] = false;
+        if (P.sparse[l]) {
+            const SplitPlan sp = plan_split(d, B, nullptr);
+            P.wants_xt[l] = sp.use ? !sp.direct : !xlds_plan(d, B, nullptr).use;
+        }
         if (l + 1 < L) P.act_bytes = std::max<size_t>(P.act_bytes, (size_t)4 * P.Bp * (size_t)d->m);
     }
     P.act_bytes = (P.act_bytes + 255) / 256 * 256;
@@ -1937,6 +1948,13 @@ extern "C" int hac_forward(const hac_layer_t* layers, uint32_t n_layers, const f
         const uint32_t relu = ly.activation == HAC_ACT_RELU ? 1u : 0u;
         if (d->format == HAC_FORMAT_IM) {
             rc = im_dot_impl(d, ly.d_blob, in, B, ld_in, out, ld_out, scratch, P.scratch_bytes, stream, ly.d_bias, relu);
+        } else if (is_mx(d)) {
+            rc = hac_internal::mx_layer(d, ly.d_blob, in, B, ld_in, out, ld_out, scratch, P.scratch_bytes, stream);
+            if (!rc) {
+                launch_bias_act(out, (uint32_t)B, (uint32_t)d->m, (uint64_t)ld_out, ly.d_bias, relu, static_cast<hipStream_t>(stream));
+                const hipError_t e = hipGetLastError();
+                if (e != hipSuccess) rc = hip_fail(e);
+            }
         } else {
             const ChainIO io = { fed ? in : nullptr, feeds ? out : nullptr, ly.d_bias, relu };
             rc = dot_impl(d->format, d, ly.d_blob, in, B, ld_in, out, ld_out, scratch, P.scratch_bytes, nullptr, stream, &io);

@@ -21,12 +21,12 @@ using namespace hac_internal;
 namespace {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef f32x4 f32x4u __attribute__((aligned(4)));                  // global memory takes 128-bit loads at any element
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef u32x4 u32x4u __attribute__((aligned(2)));
+typedef u32x4 word4 __attribute__((aligned(4)));                   // global memory takes 128-bit loads at any word
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 #define ALWAYS_INLINE __attribute__((always_inline))
@@ -46,25 +46,108 @@ __device__ __forceinline__ bf16x2 pair(uint32_t word) { return __builtin_bit_cas
 
 // ---- 32 entries of a row of X ------------------------------------------------------------
 
+// Exchanges lane bit 5 (4) with the choice between two registers: a keeps its lower half (even rows of 16 lanes) and gets b's as its upper half.
+__device__ __forceinline__ void swap32(uint32_t& a, uint32_t& b)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+    a = r[0]; b = r[1];
+}
+__device__ __forceinline__ void swap16(uint32_t& a, uint32_t& b)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(a, b, false, false);
+    a = r[0]; b = r[1];
+}
+
+// load_step: lane 16 g + c has row c and wants its entries 32 g ... of a step of 128.  Read that way, a load of 16 bytes a lane touches 64 lines; so
+// the four lanes of a row read 64 bytes side by side and then exchange pieces.
+// 16 bytes of a row from any entry on.  Loads that start at a word are as quick as aligned ones, loads that start inside a word several times
+// slower; so where rows of bfloat16 may (not `words`), the words that hold the entries are read and shifted.  A word that holds an entry is
+// readable as a whole.
+template <typename T> __device__ __forceinline__ bool whole_words(const T* X, uint64_t ldx)      // every row begins at a word
+{
+    return sizeof(T) == 4 || ((reinterpret_cast<uintptr_t>(X) | 2 * ldx) & 3) == 0;
+}
+__device__ __forceinline__ u32x4 load16(const float* p, bool) { return *reinterpret_cast<const word4*>(p); }
+__device__ __forceinline__ u32x4 load16(const __bf16* p, bool words)
+{
+    if (words) return *reinterpret_cast<const word4*>(p);
+    const uintptr_t at = reinterpret_cast<uintptr_t>(p), odd = at & 2;
+    const u32x4 q = *reinterpret_cast<const word4*>(at - odd);
+    const uint32_t e = *reinterpret_cast<const uint32_t*>(at - odd + (odd ? 16 : 12));
+    return odd ? u32x4{q.x >> 16 | q.y << 16, q.y >> 16 | q.z << 16, q.z >> 16 | q.w << 16, q.w >> 16 | e << 16} : q;
+}
+
+// 16 bytes from entry k of a step on, of which the row has `left` entries, zeros behind: the row's last 16 bytes, moved down by the entries that
+// come before k, where they end first.  One load whatever k is, so that no lane waits for another's.  (A row of less than 16 bytes: entry by entry.)
+template <typename T> __device__ __forceinline__ u32x4 piece_of(const T* row, uint32_t k, uint32_t left, uint32_t n, bool words)
+{
+    constexpr int E = 16 / sizeof(T);
+    u32x4 p = {0, 0, 0, 0};
+    if (n < (uint32_t)E) {
+        for (uint32_t i = 0; i < (uint32_t)E && k + i < left; ++i) {
+            if constexpr (E == 4) { if (i == 0) p.x = __float_as_uint(row[k]); else if (i == 1) p.y = __float_as_uint(row[k + 1]); else p.z = __float_as_uint(row[k + 2]); }
+            else {
+                const uint32_t v = (uint32_t)reinterpret_cast<const uint16_t*>(row)[k + i] << (16 * (i & 1));
+                if (i < 2) p.x |= v; else if (i < 4) p.y |= v; else if (i < 6) p.z |= v; else p.w |= v;
+            }
+        }
+        return p;
+    }
+    const int at = min((int)k, (int)left - E), d = (int)k - at;      // (at may lie before the step, never before the row)
+    p = load16(row + at, words);
+    if constexpr (E == 8) {
+        if (d & 1) p = u32x4{p.x >> 16 | p.y << 16, p.y >> 16 | p.z << 16, p.z >> 16 | p.w << 16, p.w >> 16};
+    }
+    const int moved = d / (E / 4);                                  // in words
+    if (moved & 1) p = u32x4{p.y, p.z, p.w, 0};
+    if (moved & 2) p = u32x4{p.z, p.w, 0, 0};
+    if (moved >= 4) p = u32x4{0, 0, 0, 0};
+    return p;
+}
+
 template <typename T> struct Block32;
 template <> struct Block32<float> {
     f32x4 v[8];
-    __device__ __forceinline__ void load(const float* p)
+    __device__ __forceinline__ void load_step(const float* row, uint32_t g, bool words)
     {
+        u32x4 p[8];                                                  // piece 4 i + g of the row's 32
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = *reinterpret_cast<const f32x4u*>(p + 4 * i);
+        for (int i = 0; i < 8; ++i) p[i] = load16(row + 16 * i + 4 * g, words);
+        exchange(p);
     }
-    __device__ __forceinline__ void load_part(const float* p, int32_t left)       // the first `left` entries, zeros behind
+    __device__ __forceinline__ void load_step(const float* row, uint32_t g, bool words, uint32_t left, uint32_t n)      // ... of which the first `left` are there
+    {
+        u32x4 p[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) p[i] = piece_of(row, 16 * i + 4 * g, left, n, words);
+        exchange(p);
+    }
+    __device__ __forceinline__ void exchange(u32x4* p)
     {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) v[i / 4][i % 4] = i < left ? p[i] : 0.0f;
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { uint32_t a = p[i][e], b = p[i + 4][e]; swap32(a, b); p[i][e] = a; p[i + 4][e] = b; }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (i & 2) continue;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { uint32_t a = p[i][e], b = p[i + 2][e]; swap16(a, b); p[i][e] = a; p[i + 2][e] = b; }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = __builtin_bit_cast(f32x4, p[(i & 2) << 1 | (i & 1) << 1 | i >> 2]);   // (register 4 p1 + 2 p0 + p2 has piece 8 g + 4 p2 + 2 p1 + p0)
     }
     __device__ __forceinline__ uint32_t most() const                             // bits of the largest magnitude
     {
-        uint32_t a = 0;
+        // (as integers the largest of the positive ones, and of all: a negative one's pattern is above every positive one's)
+        int32_t up = 0;
+        uint32_t any = 0;
 #pragma unroll
-        for (int i = 0; i < 32; ++i) a = max(a, __float_as_uint(v[i / 4][i % 4]) & 0x7fffffffu);
-        return a;
+        for (int i = 0; i < 32; ++i) {
+            up = max(up, (int32_t)__float_as_uint(v[i / 4][i % 4]));
+            any = max(any, __float_as_uint(v[i / 4][i % 4]));
+        }
+        return max((uint32_t)up, any & 0x7fffffffu);
     }
     __device__ __forceinline__ u32x4 codes(float scale) const
     {
@@ -103,29 +186,38 @@ template <> struct Block32<float> {
 };
 template <> struct Block32<__bf16> {
     u32x4 v[4];
-    __device__ __forceinline__ void load(const __bf16* p)
+    __device__ __forceinline__ void load_step(const __bf16* row, uint32_t g, bool words)
     {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const u32x4u*>(p + 8 * i);
+        for (int i = 0; i < 4; ++i) v[i] = load16(row + 32 * i + 8 * g, words);       // piece 4 i + g of 16
+        exchange();
     }
-    __device__ __forceinline__ void load_part(const __bf16* p, int32_t left)
+    __device__ __forceinline__ void load_step(const __bf16* row, uint32_t g, bool words, uint32_t left, uint32_t n)
     {
-        const uint16_t* q = reinterpret_cast<const uint16_t*>(p);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const uint32_t lo = 2 * i < left ? q[2 * i] : 0u, hi = 2 * i + 1 < left ? q[2 * i + 1] : 0u;
-            v[i / 4][i % 4] = lo | hi << 16;
-        }
+        for (int i = 0; i < 4; ++i) v[i] = piece_of(row, 32 * i + 8 * g, left, n, words);
+        exchange();
+    }
+    __device__ __forceinline__ void exchange()
+    {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { uint32_t a = v[i][e], b = v[i + 2][e]; swap32(a, b); v[i][e] = a; v[i + 2][e] = b; }
+#pragma unroll
+        for (int i = 0; i < 4; i += 2)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { uint32_t a = v[i][e], b = v[i + 1][e]; swap16(a, b); v[i][e] = a; v[i + 1][e] = b; }
     }
     __device__ __forceinline__ uint32_t most() const
     {
-        uint32_t a = 0;
+        u16x2 a = {0, 0};
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            const uint32_t w = v[i / 4][i % 4];
-            a = max(a, max(w << 16 & 0x7fff0000u, w & 0x7fff0000u));
+            const uint32_t w = v[i / 4][i % 4] & 0x7fff7fffu;
+            a = __builtin_elementwise_max(a, __builtin_bit_cast(u16x2, w));
         }
-        return a;
+        return (uint32_t)max(a.x, a.y) << 16;
     }
     __device__ __forceinline__ u32x4 codes(float scale) const
     {
@@ -306,124 +398,118 @@ mx_decode_kernel(T* __restrict__ W, uint64_t ldw, uint64_t stride, MxW w)
         if ((uint32_t)i < rows) p[(uint64_t)i * ldw] = (T)(byte == 255 ? __builtin_nanf("") : v[i]);
 }
 
-// ---- few rows ----------------------------------------------------------------------------------
-// At most 16 NR rows of X per group: what counts is to read W once and at once.  A block owns NC tiles of columns, its wavefronts share the
-// steps down the rows of W, each reads its tiles straight into operands; X comes from memory (from the L2 after the first block) in
-// operand order, is turned into parts or quantised by the lane that holds the block, and the wavefronts' sums are added in LDS in order.
-// A lane past the last row reads that row again: what it adds goes to sums that nobody stores.
-template <int MODE, typename T, int NR, int NC, int U>
+// ---- few rows, or little work ------------------------------------------------------------------
+// 16 rows of X at a time: what counts is to have everything in flight at once and to launch one kernel.  A block owns 16 rows and NC tiles of
+// columns (and, with splits, a range of k), its wavefronts share the steps, each reads its tiles of W straight into operands; X comes from memory
+// (from the L2 after the first block), is turned into parts or quantised by the lane that holds the block, and the wavefronts' sums are
+// added in LDS in order.  A lane past the last row reads that row again: what it adds goes to sums that nobody stores.
+template <int MODE, typename T, int NC, int U>
 __global__ void __launch_bounds__(512)
 mx_rows_kernel(MxW w, const T* __restrict__ X, uint64_t ldx, uint32_t B, const int32_t* __restrict__ offsets,
-               T* __restrict__ Y, uint64_t ldy, uint32_t col_blocks)
+               T* __restrict__ Y, uint64_t ldy, uint32_t each, uint32_t more, float* __restrict__ part)
 {
-    extern __shared__ __align__(16) f32x4 red[];                 // [wavefronts][NR * NC][64]
-    const uint32_t lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+    extern __shared__ __align__(16) f32x4 red[];                 // [wavefronts][NC][64]
+    const uint32_t lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4, lane16 = 16 * lane, lane4 = 4 * lane;
     const uint32_t wave = uniform(threadIdx.x >> 6), waves = blockDim.x >> 6;
-    const uint32_t stretch = blockIdx.x / col_blocks, cb = blockIdx.x - stretch * col_blocks;
-    const Item it = find_item(offsets, w.count, B, 16 * NR, stretch);
+    const uint32_t cb = blockIdx.x, split = blockIdx.z, splits = gridDim.z;
+    const Item it = find_item(offsets, w.count, B, 16, blockIdx.y);
     if (!it.rows) return;
-    const uint32_t s0 = (uint32_t)((uint64_t)w.steps * wave / waves), s1 = (uint32_t)((uint64_t)w.steps * (wave + 1) / waves);
-    const uint32_t full = min(s1, w.n / 128);
+    // every wavefront of every split has `each` steps, the first `more` of them one more
+    const uint32_t share = split * waves + wave, s0 = share * each + min(share, more), s1 = s0 + each + (share < more ? 1u : 0u);
     const uint8_t* code[NC];
     const uint8_t* scale[NC];
 #pragma unroll
     for (int q = 0; q < NC; ++q) {
         const uint32_t ct = min(cb * NC + q, w.ctiles - 1);
-        code[q] = w.codes + it.expert * w.code_stride + (uint64_t)ct * w.steps * 1024 + 16 * lane;
-        scale[q] = w.scales + it.expert * w.scale_stride + (uint64_t)ct * w.groups * 256 + 4 * lane;
+        code[q] = w.codes + it.expert * w.code_stride + (uint64_t)ct * w.steps * 1024;
+        scale[q] = w.scales + it.expert * w.scale_stride + (uint64_t)ct * w.groups * 256;
     }
-    const T* row[NR];
+    const T* row = X + (uint64_t)(it.row0 + min(c, it.rows - 1)) * ldx;
+    const bool words = whole_words(X, ldx);
+    f32x4 acc[NC];
 #pragma unroll
-    for (int r = 0; r < NR; ++r) row[r] = X + (uint64_t)(it.row0 + min(16u * r + c, it.rows - 1)) * ldx + 32 * g;
-    f32x4 acc[NR][NC];
-#pragma unroll
-    for (int r = 0; r < NR; ++r)
-#pragma unroll
-        for (int q = 0; q < NC; ++q) acc[r][q] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int q = 0; q < NC; ++q) acc[q] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
-    auto multiply = [&](const Block32<T>* x, const u32x4* code4, const uint32_t* byte) ALWAYS_INLINE {
+    auto load_w = [&](uint32_t step, u32x4* codes, uint32_t* byte) ALWAYS_INLINE {
+#pragma unroll
+        for (int q = 0; q < NC; ++q) {
+            codes[q] = *reinterpret_cast<const u32x4*>(code[q] + (uint64_t)step * 1024 + lane16);
+            byte[q] = *(scale[q] + (uint64_t)(step / 4) * 256 + step % 4 + lane4);
+        }
+    };
+    auto multiply = [&](const Block32<T>& x, const u32x4* codes, const uint32_t* byte) ALWAYS_INLINE {
         if constexpr (MODE == FP4) {
+            uint32_t xs;
+            const u32x4 xc = quantise(x, xs);
 #pragma unroll
-            for (int r = 0; r < NR; ++r) {
-                uint32_t xs;
-                const u32x4 xc = quantise(x[r], xs);
-#pragma unroll
-                for (int q = 0; q < NC; ++q) acc[r][q] = multiply_fp4<0>(code4[q], byte[q], xc, xs, acc[r][q]);
-            }
+            for (int q = 0; q < NC; ++q) acc[q] = multiply_fp4<0>(codes[q], byte[q], xc, xs, acc[q]);
         } else {
-            constexpr int P = MODE;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                u32x4 p[NR][P];
-#pragma unroll
-                for (int r = 0; r < NR; ++r) x[r].parts(j, p[r]);
+                u32x4 p[MODE];
+                x.parts(j, p);
 #pragma unroll
                 for (int q = 0; q < NC; ++q) {
-                    const bf16x8 v = weights(code4[q][j], scale_of(byte[q]));
+                    const bf16x8 v = weights(codes[q][j], scale_of(byte[q]));
 #pragma unroll
-                    for (int r = 0; r < NR; ++r)
-#pragma unroll
-                        for (int i = P - 1; i >= 0; --i) acc[r][q] = multiply_bf16(v, p[r][i], acc[r][q]);
+                    for (int i = MODE - 1; i >= 0; --i) acc[q] = multiply_bf16(v, p[i], acc[q]);
                 }
             }
         }
     };
-    uint32_t s = s0;
-    for (; s + U <= full; s += U) {
-        Block32<T> x[U][NR];
-        u32x4 code4[U][NC];
+    // U steps at a time are requested before the first is multiplied (behind the last: that one again, not multiplied)
+    const uint32_t full = min(s1, w.n / 128);
+    for (uint32_t s = s0; s < full; s += U) {
+        Block32<T> x[U];
+        u32x4 codes[U][NC];
         uint32_t byte[U][NC];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-#pragma unroll
-            for (int q = 0; q < NC; ++q) {
-                code4[u][q] = *reinterpret_cast<const u32x4*>(code[q] + (uint64_t)(s + u) * 1024);
-                byte[u][q] = scale[q][(uint64_t)((s + u) / 4) * 256 + (s + u) % 4];
-            }
-#pragma unroll
-            for (int r = 0; r < NR; ++r) x[u][r].load(row[r] + (uint64_t)(s + u) * 128);
+            const uint32_t step = min(s + u, full - 1);
+            load_w(step, codes[u], byte[u]);
+            x[u].load_step(row + (uint64_t)step * 128, g, words);
         }
 #pragma unroll
-        for (int u = 0; u < U; ++u) multiply(x[u], code4[u], byte[u]);
+        for (int u = 0; u < U; ++u) {
+            if (s + u >= full) break;
+            multiply(x[u], codes[u], byte[u]);
+        }
     }
-    for (; s < s1; ++s) {
-        Block32<T> x[NR];
-        u32x4 code4[NC];
+    if (max(full, s0) < s1) {                                    // a last step that is not whole
+        Block32<T> x;
+        u32x4 codes[NC];
         uint32_t byte[NC];
-#pragma unroll
-        for (int q = 0; q < NC; ++q) {
-            code4[q] = *reinterpret_cast<const u32x4*>(code[q] + (uint64_t)s * 1024);
-            byte[q] = scale[q][(uint64_t)(s / 4) * 256 + s % 4];
-        }
-#pragma unroll
-        for (int r = 0; r < NR; ++r) {
-            if (s < full) x[r].load(row[r] + (uint64_t)s * 128);
-            else x[r].load_part(row[r] + (uint64_t)s * 128, (int32_t)w.n - (int32_t)(s * 128 + 32 * g));
-        }
-        multiply(x, code4, byte);
+        load_w(s1 - 1, codes, byte);
+        x.load_step(row + (uint64_t)(s1 - 1) * 128, g, words, w.n - (s1 - 1) * 128, w.n);
+        multiply(x, codes, byte);
     }
-    const bool wide = (reinterpret_cast<uintptr_t>(Y) | ldy * sizeof(T)) % (4 * sizeof(T)) == 0;
-    auto put = [&](uint32_t r, uint32_t q, uint32_t l, f32x4 v) ALWAYS_INLINE {
-        const uint32_t at = 16 * r + (l & 15), col = (cb * NC + q) * 16 + 4 * (l >> 4);
-        if (at < it.rows && col < w.m) store4(Y + (uint64_t)(it.row0 + at) * ldy, col, w.m, wide, v);
-    };
 #pragma unroll
-    for (int r = 0; r < NR; ++r)
-#pragma unroll
-        for (int q = 0; q < NC; ++q) red[((size_t)wave * NR * NC + r * NC + q) * 64 + lane] = acc[r][q];
+    for (int q = 0; q < NC; ++q) red[((size_t)wave * NC + q) * 64 + lane] = acc[q];
     __syncthreads();
-    for (uint32_t o = threadIdx.x; o < NR * NC * 64; o += blockDim.x) {
+    const bool wide = (reinterpret_cast<uintptr_t>(Y) | ldy * sizeof(T)) % (4 * sizeof(T)) == 0;
+    for (uint32_t o = threadIdx.x; o < NC * 64; o += blockDim.x) {
         f32x4 v = red[o];
-        for (uint32_t z = 1; z < waves; ++z) v += red[(size_t)z * NR * NC * 64 + o];
-        put(o / 64 / NC, o / 64 % NC, o & 63, v);
+        for (uint32_t z = 1; z < waves; ++z) v += red[(size_t)z * NC * 64 + o];
+        const uint32_t at = o & 15, col = (cb * NC + o / 64) * 16 + 4 * ((o & 63) >> 4);
+        if (at >= it.rows || col >= w.m) continue;
+        if (splits == 1) store4(Y + (uint64_t)(it.row0 + at) * ldy, col, w.m, wide, v);
+        else store4(part + ((uint64_t)split * B + it.row0 + at) * w.m, col, w.m, w.m % 4 == 0, v);
     }
 }
 
 // ---- many rows -----------------------------------------------------------------------------------
-// X is first written in operand order, group by group, each group from a tile of 16 rows of its own on: quantised codes (and their
-// scales in groups of four tiles, as W's), or bf16 parts, [tile][step][part][operand j][lane][16 bytes]; zeros behind entry n.
+// X in operand order, group by group, each group from a tile of 16 rows of its own on, zeros behind entry n: quantised codes (and
+// their scales in groups of four tiles, as W's); bf16 rows as [tile][step][row][piece of 8 k], pieces in an order that differs from
+// row to row (turned); the three parts of fp32 rows as [tile][step][half][part][operand][lane][16 bytes].
 // (A wavefront has a tile's step, a lane a block of its row.)
+template <int MODE> __host__ __device__ constexpr uint32_t chunk_bytes()          // of 16 rows: what is staged at once
+{
+    return MODE == FP4 ? 4096u + 256u : MODE == ONE ? 4096u : 6144u;
+}
 __host__ __device__ constexpr uint32_t step_bytes(int mode) { return mode == FP4 ? 1024u : 4096u * mode; }
+// where a piece of a row lies: any 16 lanes that LDS serves at a time (0 .. 3, 12 .. 15, 20 .. 27 and so on) read from 16 different ones
+__device__ __forceinline__ uint32_t turned(uint32_t row, uint32_t piece) { return piece ^ ((row & 3) | ((0u - row / 4) & 3) << 2); }
+__device__ __forceinline__ uint32_t place(uint32_t row, uint32_t piece) { return row * 256 + turned(row, piece) * 16; }
 
 template <int MODE, typename T>
 __global__ void __launch_bounds__(256)
@@ -437,10 +523,10 @@ mx_lay_out_kernel(const T* __restrict__ X, uint64_t ldx, uint32_t n, uint32_t st
     const Item it = find_item(offsets, count, B, 16, tile);
     if (!it.rows) return;
     const T* row = X + (uint64_t)(it.row0 + min(c, it.rows - 1)) * ldx;
-    const uint32_t k = step * 128 + 32 * g;
+    const bool words = whole_words(X, ldx);
     Block32<T> x;
-    if (k + 32 <= n) x.load(row + k);
-    else x.load_part(row + k, k < n ? (int32_t)(n - k) : 0);
+    if (step * 128 + 128 <= n) x.load_step(row + step * 128, g, words);
+    else x.load_step(row + step * 128, g, words, n > step * 128 ? n - step * 128 : 0u, n);
     if constexpr (MODE == FP4) {                             // steps: 4 * groups
         uint32_t byte;
         const u32x4 q = quantise(x, byte);
@@ -451,35 +537,59 @@ mx_lay_out_kernel(const T* __restrict__ X, uint64_t ldx, uint32_t n, uint32_t st
             reinterpret_cast<uint32_t*>(out_scales)[((uint64_t)tile * groups + blockIdx.y) * 64 + lane] = reinterpret_cast<const uint32_t*>(bytes)[lane];
     } else {
         if (step >= steps) return;
+        uint8_t* to = out + ((uint64_t)tile * steps + step) * step_bytes(MODE);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             u32x4 p[MODE];
             x.parts(j, p);
+            if constexpr (MODE == ONE) *reinterpret_cast<u32x4*>(to + place(c, 4 * g + j)) = p[0];
+            else
 #pragma unroll
-            for (int i = 0; i < MODE; ++i)
-                *reinterpret_cast<u32x4*>(out + (((((uint64_t)tile * steps + step) * MODE + i) * 4 + j) * 64 + lane) * 16) = p[i];
+                for (int i = 0; i < 3; ++i) *reinterpret_cast<u32x4*>(to + ((j / 2 * 3 + i) * 2 + j % 2) * 1024 + lane * 16) = p[i];
         }
     }
 }
 
 // The product.  A block of 4 wavefronts owns 16 NR rows x 64 NC columns, wavefront w the 16 NC columns from 16 NC w on and all rows.
-// A chunk (a step of 128 k; four of them for codes) of X goes to LDS as it lies in memory, one chunk ahead, past the registers; a column
-// belongs to one wavefront, so W goes from memory into its registers, a chunk ahead too, and is expanded once per block.
-template <int MODE> __host__ __device__ constexpr uint32_t chunk_bytes() { return MODE == FP4 ? 4096u + 256u : step_bytes(MODE); }
+// A chunk of X (a step of 128 k; half of one as three parts; four of them as codes) goes to LDS past the registers, one chunk ahead; a
+// column belongs to one wavefront, so W goes from memory into its registers, ahead too, and is expanded once per block.
+// The order of a chunk is spelled out in beats of NC matrix instructions: left to itself the compiler reads an operand right before its
+// use and waits.  A beat's operand of X is read two beats ahead, and W's operands of the next 32 k are expanded beside this one's products.
+// DIRECT: bf16 rows whose pieces of 8 k are whole and aligned need no laying out, they are staged from where they are.
+__device__ __constant__ uint32_t zeros16[4] = {0, 0, 0, 0};
 
-__device__ __forceinline__ void to_lds(const uint8_t* from, uint8_t* lds, bool word)
+// 16 bytes (4) a lane from memory to lds + 16 (4) * lane, past the registers.  In assembly, so that the compiler counts its own loads only: with
+// these among them it waits for everything in flight wherever it needs one load or one read of LDS.  A wait for its own loads waits for these too
+// then, never the other way round: loads_done() is what says that they are.
+__device__ __forceinline__ uint32_t lds_offset(const uint8_t* p) { return uniform((uint32_t)(uintptr_t)(const __attribute__((address_space(3))) uint8_t*)p); }
+__device__ __forceinline__ void to_lds(const void* from, const uint8_t* lds)
 {
-    if (word) __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)lds, 4, 0, 0);
-    else __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)lds, 16, 0, 0);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_offset(lds)), "v"(from) : "memory", "m0");
+}
+__device__ __forceinline__ void to_lds(const void* base, uint32_t offset, const uint8_t* lds)      // (base: the wavefront's)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_offset(lds)), "v"(offset), "s"(base) : "memory", "m0");
+}
+__device__ __forceinline__ void word_to_lds(const void* base, uint32_t offset, const uint8_t* lds)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds_offset(lds)), "v"(offset), "s"(base) : "memory", "m0");
+}
+__device__ __forceinline__ void loads_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ void block_sync_lds()                                  // loads from global memory stay in flight across it
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
-template <int MODE, typename T, int NR, int NC>
+template <int MODE, bool DIRECT, typename T, int NR, int NC>
 __global__ void __launch_bounds__(256, 2)
-mx_tile_kernel(MxW w, const uint8_t* __restrict__ xt, const uint8_t* __restrict__ xs, uint32_t max_tiles, uint32_t B,
-               const int32_t* __restrict__ offsets, T* __restrict__ Y, uint64_t ldy, uint32_t stretches, uint32_t col_blocks,
-               uint32_t splits, uint32_t per_split, float* __restrict__ part)
+mx_tile_kernel(MxW w, const uint8_t* __restrict__ xt, const uint8_t* __restrict__ xs, uint64_t ldx, uint32_t max_tiles, uint32_t B,
+               const int32_t* __restrict__ offsets, T* __restrict__ Y, uint64_t ldy, uint32_t rows_each, uint32_t stretches,
+               uint32_t col_blocks, uint32_t splits, uint32_t per_split, float* __restrict__ part)
 {
     constexpr uint32_t CH = chunk_bytes<MODE>(), STAGE = NR * CH;
+    constexpr int HALVES = MODE == THREE ? 2 : 1, WS = MODE == FP4 ? 4 : 1;      // chunks of a step; steps of a chunk
     extern __shared__ __align__(16) uint8_t lds[];               // two stages
     const uint32_t lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
     // consecutive items on one XCD; the stretches of a column block follow one another and share its part of W in that L2
@@ -487,10 +597,10 @@ mx_tile_kernel(MxW w, const uint8_t* __restrict__ xt, const uint8_t* __restrict_
     if (id >= stretches * col_blocks * splits) return;
     const uint32_t split = id / (stretches * col_blocks), rest = id - split * stretches * col_blocks;
     const uint32_t cb = rest / stretches, stretch = rest - cb * stretches;
-    const Item it = find_item(offsets, w.count, B, 16 * NR, stretch);
+    const Item it = find_item(offsets, w.count, B, rows_each, stretch);
     const uint32_t tiles = (it.rows + 15) / 16;
-    if (!it.rows || it.tile + tiles > max_tiles) return;
-    const uint32_t chunks = MODE == FP4 ? w.groups : w.steps;
+    if (!it.rows || (!DIRECT && it.tile + tiles > max_tiles)) return;
+    const uint32_t chunks = MODE == FP4 ? w.groups : w.steps;    // (a step, or a group of four)
     const uint32_t c0 = split * per_split, c1 = min(chunks, c0 + per_split);
 
     const uint8_t* code[NC];
@@ -498,100 +608,155 @@ mx_tile_kernel(MxW w, const uint8_t* __restrict__ xt, const uint8_t* __restrict_
 #pragma unroll
     for (int q = 0; q < NC; ++q) {
         const uint32_t ct = min((cb * 4 + wave) * NC + q, w.ctiles - 1);
-        code[q] = w.codes + it.expert * w.code_stride + (uint64_t)ct * w.steps * 1024 + 16 * lane;
-        scale[q] = w.scales + it.expert * w.scale_stride + (uint64_t)ct * w.groups * 256 + 4 * lane;
+        code[q] = w.codes + it.expert * w.code_stride + (uint64_t)ct * w.steps * 1024;       // (the wavefront's: lanes add 16 and 4 bytes each)
+        scale[q] = w.scales + it.expert * w.scale_stride + (uint64_t)ct * w.groups * 256;
     }
+    const uint32_t lane16 = 16 * lane, lane4 = 4 * lane;
     // pieces of 1024 bytes (and of 256 for the scales) are dealt to the wavefronts; rows past the last tile keep what LDS holds
-    auto stage = [&](uint32_t ch, uint32_t buf) ALWAYS_INLINE {
-        uint8_t* to = lds + buf * STAGE;
-        constexpr uint32_t PIECES = (MODE == FP4 ? 4096u : CH) / 1024;
-        for (uint32_t z = wave; z < NR * PIECES; z += 4) {
-            const uint32_t t = z / PIECES, p = z - t * PIECES;
-            if (t >= tiles) break;
-            const uint64_t at = MODE == FP4 ? ((uint64_t)(it.tile + t) * w.groups + ch) * 4096 : ((uint64_t)(it.tile + t) * w.steps + ch) * CH;
-            to_lds(xt + at + p * 1024 + lane * 16, to + t * (PIECES * 1024) + p * 1024, false);
+    const uint32_t row4 = 4 * wave + lane / 16, piece = turned(row4, lane & 15);
+    const uint8_t *first = nullptr, *end = nullptr;              // DIRECT: a lane's row of the first tile and, the last row again, of the last
+    if constexpr (DIRECT) {
+        first = xt + ((uint64_t)(it.row0 + min(row4, it.rows - 1)) * ldx + 8 * piece) * 2;
+        end = xt + ((uint64_t)(it.row0 + min(16 * (tiles - 1) + row4, it.rows - 1)) * ldx + 8 * piece) * 2;
+    }
+    auto stage = [&](auto count, uint32_t ch, uint32_t half, uint8_t* to) ALWAYS_INLINE {
+        constexpr uint32_t N = decltype(count)::value;
+        if constexpr (DIRECT) {
+            const bool inside = ch * 128 + 8 * piece < w.n;
+#pragma unroll
+            for (uint32_t t = 0; t < N; ++t) {
+                const uint8_t* from = (t + 1 < tiles ? first + t * (32 * ldx) : end) + (uint64_t)ch * 256;
+                to_lds(inside ? from : reinterpret_cast<const uint8_t*>(zeros16), to + t * 4096 + wave * 1024);
+            }
+        } else {
+            constexpr uint32_t PIECES = (MODE == FP4 ? 4096u : CH) / 1024;
+#pragma unroll
+            for (uint32_t i = 0; i < (N * PIECES + 3) / 4; ++i) {
+                const uint32_t z = wave + 4 * i, t = z / PIECES, p = z - t * PIECES;
+                if (N * PIECES % 4 && z >= N * PIECES) break;
+                const uint64_t at = ((uint64_t)(it.tile + min(t, tiles - 1)) * chunks + ch) * (MODE == FP4 ? 4096 : step_bytes(MODE)) + half * CH;
+                to_lds(xt + at + p * 1024, lane16, to + t * (PIECES * 1024) + p * 1024);
+            }
+            if constexpr (MODE == FP4)
+                for (uint32_t t = wave; t < N; t += 4)
+                    word_to_lds(xs + ((uint64_t)(it.tile + min(t, tiles - 1)) * w.groups + ch) * 256, lane4, to + NR * 4096 + t * 256);
         }
-        if constexpr (MODE == FP4)
-            for (uint32_t t = wave; t < tiles; t += 4)
-                to_lds(xs + ((uint64_t)(it.tile + t) * w.groups + ch) * 256 + lane * 4, to + NR * 4096 + t * 256, true);
     };
     f32x4 acc[NR][NC];
 #pragma unroll
     for (int r = 0; r < NR; ++r)
 #pragma unroll
         for (int q = 0; q < NC; ++q) acc[r][q] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    uint32_t at_lane[4];                                         // of a lane's operand in LDS
+#pragma unroll
+    for (int j = 0; j < 4; ++j) at_lane[j] = MODE == ONE ? place(lane & 15, 4 * (lane >> 4) + j) : lane16;
 
-    constexpr int WS = MODE == FP4 ? 4 : 1;                      // steps of a chunk
-    u32x4 cur[WS][NC];
-    uint32_t cur_s[NC];
-    auto load_w = [&](uint32_t ch, u32x4 (&to)[WS][NC], uint32_t* to_s) ALWAYS_INLINE {
+    // steps s of chunk ch (behind the last step: any tile, X's codes are 0 there and W's scales too)
+    auto load_codes = [&](uint32_t ch, int s, u32x4 (&to)[NC]) ALWAYS_INLINE {
+        const uint32_t step = MODE == FP4 ? min(ch * 4 + s, w.steps - 1) : ch;
+#pragma unroll
+        for (int q = 0; q < NC; ++q) to[q] = *reinterpret_cast<const u32x4*>(code[q] + (uint64_t)step * 1024 + lane16);
+    };
+    auto load_scales = [&](uint32_t ch, uint32_t* to) ALWAYS_INLINE {
 #pragma unroll
         for (int q = 0; q < NC; ++q) {
-            if constexpr (MODE == FP4) {
-                to_s[q] = *reinterpret_cast<const uint32_t*>(scale[q] + (uint64_t)ch * 256);
+            if constexpr (MODE == FP4) to[q] = *reinterpret_cast<const uint32_t*>(scale[q] + (uint64_t)ch * 256 + lane4);
+            else to[q] = *(scale[q] + (uint64_t)(ch / 4) * 256 + ch % 4 + lane4);
+        }
+    };
+
+    // the chunks with the first N of the NR tiles of rows
+    auto walk = [&](auto count) ALWAYS_INLINE {
+        constexpr int N = decltype(count)::value;
+        u32x4 cur[WS][NC], next[NC];
+        uint32_t cur_s[NC], next_s[NC];
+        bf16x8 v[2][NC];                                         // W's operand of these 32 k and the next
+        const uint32_t last = (c1 - c0) * HALVES - 1;            // chunk u: step c0 + u / HALVES, half u % HALVES
+        stage(count, c0, 0, lds);
+        load_scales(c0, cur_s);
 #pragma unroll
-                for (int s = 0; s < WS; ++s)                     // (behind the last step: any tile, X's codes are 0 there and W's scales too)
-                    to[s][q] = *reinterpret_cast<const u32x4*>(code[q] + (uint64_t)min(ch * 4 + s, w.steps - 1) * 1024);
-            } else {
-                to_s[q] = scale[q][(uint64_t)(ch / 4) * 256 + ch % 4];
-                to[0][q] = *reinterpret_cast<const u32x4*>(code[q] + (uint64_t)ch * 1024);
+        for (int s = 0; s < WS; ++s) load_codes(c0, s, cur[s]);
+        if constexpr (MODE != FP4) {
+#pragma unroll
+            for (int q = 0; q < NC; ++q) v[0][q] = weights(cur[0][q][0], scale_of(cur_s[q]));
+        }
+        loads_done();
+        uint32_t u = 0;
+        for (uint32_t ch = c0; ch < c1; ++ch) {
+            const uint32_t ahead = min(ch + 1, c1 - 1);
+#pragma unroll
+            for (int half = 0; half < HALVES; ++half) {
+                const uint8_t* x = lds + (u & 1) * STAGE;
+                block_sync_lds();                                // all have their part of this chunk, and have read the one before
+                if (half == 0) {
+                    load_scales(ahead, next_s);
+                    if constexpr (MODE != FP4) load_codes(ahead, 0, next);
+                }
+                if (u < last) stage(count, c0 + (u + 1) / HALVES, (u + 1) % HALVES, lds + (~u & 1) * STAGE);
+                ++u;
+                __builtin_amdgcn_sched_barrier(0);
+                // beat b multiplies one operand of X; what it is depends on b alone
+                constexpr int PARTS = MODE == THREE ? 3 : 1, JS = 4 / HALVES, PER = N * PARTS, BEATS = JS * PER;
+                auto operand_at = [&](int b) ALWAYS_INLINE -> u32x4 {
+                    const int j = b / PER, i = PARTS - 1 - b % PER / N, r = b % N;
+                    if constexpr (MODE == FP4) return *reinterpret_cast<const u32x4*>(x + r * 4096 + j * 1024 + at_lane[0]);
+                    else if constexpr (MODE == ONE) return *reinterpret_cast<const u32x4*>(x + r * 4096 + at_lane[j]);
+                    else return *reinterpret_cast<const u32x4*>(x + r * CH + (i * 2 + j) * 1024 + at_lane[0]);
+                };
+                u32x4 xq[3];
+                uint32_t sx[N];
+                xq[0] = operand_at(0);
+                if (BEATS > 1) xq[1] = operand_at(1);
+                if constexpr (MODE == FP4) {
+#pragma unroll
+                    for (int r = 0; r < N; ++r) sx[r] = *reinterpret_cast<const uint32_t*>(x + NR * 4096 + r * 256 + lane * 4);
+                }
+#pragma unroll
+                for (int b = 0; b < BEATS; ++b) {
+                    const int j = b / PER, t = b % PER, r = b % N;
+                    if (b + 2 < BEATS) xq[(b + 2) % 3] = operand_at(b + 2);
+                    if constexpr (MODE == FP4) {
+#pragma unroll
+                        for (int q = 0; q < NC; ++q) {
+                            if (j == 0) acc[r][q] = multiply_fp4<0>(cur[0][q], cur_s[q], xq[b % 3], sx[r], acc[r][q]);
+                            if (j == 1) acc[r][q] = multiply_fp4<1>(cur[1][q], cur_s[q], xq[b % 3], sx[r], acc[r][q]);
+                            if (j == 2) acc[r][q] = multiply_fp4<2>(cur[2][q], cur_s[q], xq[b % 3], sx[r], acc[r][q]);
+                            if (j == 3) acc[r][q] = multiply_fp4<3>(cur[3][q], cur_s[q], xq[b % 3], sx[r], acc[r][q]);
+                        }
+                    } else {
+                        const int jj = half * JS + j;            // of the step's four
+#pragma unroll
+                        for (int q = 0; q < NC; ++q) acc[r][q] = multiply_bf16(v[jj & 1][q], xq[b % 3], acc[r][q]);
+#pragma unroll
+                        for (int q = t * NC / PER; q < (t + 1) * NC / PER; ++q)
+                            v[(jj & 1) ^ 1][q] = jj < 3 ? weights(cur[0][q][(jj + 1) & 3], scale_of(cur_s[q])) : weights(next[q][0], scale_of(next_s[q]));
+                    }
+                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+#pragma unroll
+                    for (int q = 0; q < NC; ++q) {
+                        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                        __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                    // what was staged at the start of the chunk has had three quarters of it to arrive
+                    if (b == (BEATS * 3 + 3) / 4 - 1) loads_done();
+                    if (MODE == FP4 && t == PER - 1) {
+                        if (j != 1) load_codes(ahead, j, cur[j]);
+                        if (j == 2) load_codes(ahead, 1, cur[1]);
+                    }
+                }
+            }
+#pragma unroll
+            for (int q = 0; q < NC; ++q) {
+                cur_s[q] = next_s[q];
+                if constexpr (MODE != FP4) cur[0][q] = next[q];
             }
         }
     };
     if (c0 < c1) {
-        stage(c0, 0);
-        load_w(c0, cur, cur_s);
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-    }
-    for (uint32_t ch = c0; ch < c1; ++ch) {
-        const uint8_t* x = lds + ((ch - c0) & 1) * STAGE;
-        u32x4 next[WS][NC];
-        uint32_t next_s[NC];
-        const uint32_t ahead = min(ch + 1, c1 - 1);
-        load_w(ahead, next, next_s);
-        if (ch + 1 < c1) stage(ch + 1, (ch - c0 + 1) & 1);
-        if constexpr (MODE == FP4) {
-            uint32_t sx[NR];
-#pragma unroll
-            for (int r = 0; r < NR; ++r) sx[r] = *reinterpret_cast<const uint32_t*>(x + NR * 4096 + r * 256 + lane * 4);
-            auto step = [&](auto which) ALWAYS_INLINE {
-                constexpr int S = decltype(which)::value;
-#pragma unroll
-                for (int r = 0; r < NR; ++r) {
-                    const u32x4 xc = *reinterpret_cast<const u32x4*>(x + r * 4096 + S * 1024 + lane * 16);
-#pragma unroll
-                    for (int q = 0; q < NC; ++q) acc[r][q] = multiply_fp4<S>(cur[S][q], cur_s[q], xc, sx[r], acc[r][q]);
-                }
-            };
-            step(std::integral_constant<int, 0>{});
-            step(std::integral_constant<int, 1>{});
-            step(std::integral_constant<int, 2>{});
-            step(std::integral_constant<int, 3>{});
-        } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                bf16x8 v[NC];
-#pragma unroll
-                for (int q = 0; q < NC; ++q) v[q] = weights(cur[0][q][j], scale_of(cur_s[q]));
-#pragma unroll
-                for (int r = 0; r < NR; ++r)
-#pragma unroll
-                    for (int i = MODE - 1; i >= 0; --i) {
-                        const u32x4 p = *reinterpret_cast<const u32x4*>(x + r * CH + (i * 4 + j) * 1024 + lane * 16);
-#pragma unroll
-                        for (int q = 0; q < NC; ++q) acc[r][q] = multiply_bf16(v[q], p, acc[r][q]);
-                    }
-            }
-        }
-#pragma unroll
-        for (int q = 0; q < NC; ++q) {
-            cur_s[q] = next_s[q];
-#pragma unroll
-            for (int s = 0; s < WS; ++s) cur[s][q] = next[s][q];
-        }
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
+        if (NR >= 4 && tiles <= NR / 2) walk(std::integral_constant<int, NR >= 4 ? NR / 2 : NR>{});
+        else if (NR >= 4 && tiles <= NR * 3 / 4) walk(std::integral_constant<int, NR >= 4 ? NR * 3 / 4 : NR>{});
+        else walk(std::integral_constant<int, NR>{});
     }
     const uint32_t l16 = lane & 15, col0 = (cb * 4 + wave) * NC * 16 + 4 * (lane >> 4);
     const bool wide = (reinterpret_cast<uintptr_t>(Y) | ldy * sizeof(T)) % (4 * sizeof(T)) == 0;
@@ -653,108 +818,194 @@ MxW matrices(const hac_desc_t& d, const void* blob)
 
 constexpr int64_t kMostRows = 1 << 27;
 
-// What a product launches.  rows: the kernel for few rows, 16 * nr rows a stretch and nc tiles of columns a block of `waves` wavefronts; else X is
-// laid out and tiles of 16 nr rows x 64 nc columns are multiplied, the chunks of a column cut into `splits`.
+// How a product is split.  rows: the kernel for few rows, nc tiles of columns a block of `waves` wavefronts; else tiles of 16 nr rows x 64 nc
+// columns.  splits: parts that the k of a column are cut into.
+struct Choice { bool rows; uint32_t nr, nc, waves, splits; };
+
 struct Plan {
-    bool rows;
-    int mode, nr, nc;
-    uint32_t waves, splits, per_split;
+    Choice c;
+    bool direct;                                 // tiles of X as it lies
+    int mode;
+    uint32_t rows_each, per_split;               // rows a stretch; chunks a split (tiles)
     uint64_t stretches, col_blocks, tiles;       // stretches, tiles: as many as B rows in `count` groups can fill
     size_t xt_bytes, xs_bytes, part_bytes, bytes;
 };
 
+uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 uint64_t fill(uint64_t B, uint64_t count, uint64_t R) { return std::min<uint64_t>(B, (B + (R - 1) * count) / R); }
 
-Plan plan_mx(const hac_desc_t& d, uint32_t type, uint64_t B, uint32_t flags, bool grouped)
+// The split with the shortest estimate of a call's time.  Its form and constants (us) were fitted to the measured times of all splits of 260 products
+// drawn over n 64 .. 25088, m 10 .. 8192, 1 .. 12544 rows, 1 .. 64 groups: estimates are off by 10 to 19 % in the mean, and the splits they choose are
+// 2.6 % slower in the mean than the best measured ones (worst 1.35 times; the better of one split per kernel chosen by sizes alone: 45 % slower).
+//   few rows: a launch, trips to memory (two steps at a time) and what a trip grows by with each tile of columns, wavefronts beyond eight on a CU, steps
+//     of X turned into operands and steps of W multiplied per SIMD, sums stored, the pass that adds the splits and its bytes
+//   tiles: a launch, X laid out and its bytes, chunks of a block, their matrix instructions, both times the blocks of a CU, the blocks, the
+//     pass that adds the splits and its bytes, Y
+struct Costs {
+    double call, trip, trip_nc, waves, steps, steps_nc, sums, split, split_mb;
+    double t_call, t_lay, t_lay_mb, t_chunk, t_chunk_mm, t_cu_chunk, t_cu_mm, t_split, t_split_mb, t_mb;
+};
+const Costs kCosts[4] = {
+    { 4.08, 0.85, 0.06, 0.70, 0.52, 0.147, 0.06, 1.8, 6.5, 0.0, 8.02, 0.203, 0.238, 0.000, 0.053, 1.546, 1.50, 3.25, 0.61 },    // codes, from fp32
+    { 3.54, 0.84, 0.11, 0.66, 0.32, 0.080, 0.27, 2.8, 2.1, 0.0, 7.59, 0.259, 0.000, 0.557, 0.171, 1.217, 2.46, 1.69, 0.82 },    // codes, from bf16
+    { 3.40, 1.15, 0.31, 1.09, 0.57, 0.168, 0.37, 2.8, 2.2, 0.0, 8.15, 0.487, 0.206, 0.219, 0.448, 0.620, 2.13, 2.46, 1.00 },    // fp32
+    { 3.31, 0.87, 0.16, 0.36, 0.14, 0.106, 0.00, 2.1, 10., 3.65, 3.92, 0.694, 0.249, 0.344, 0.120, 0.717, 2.10, 2.04, 1.06 },    // bf16
+};
+
+Choice choose(const MxShape& s, uint64_t B, uint64_t count, uint64_t m, uint32_t type, int mode, bool direct)
+{
+    const Costs& k = kCosts[(mode == FP4 ? 0 : 2) + (type == HAC_TYPE_BF16 ? 1 : 0)];
+    const double b = (double)B, used = count > 1 ? 0.8 * (double)std::min(count, B) : 0.0, out_mb = b * (double)m / 1e6;
+    // stretches of R rows that hold rows: in groups, the last of each is half full
+    auto live = [&](uint64_t R) {
+        const uint64_t least = ceil_div(B, R);
+        return count > 1 ? std::min(b, std::max((double)least, used + b / (double)R)) : (double)least;
+    };
+    Choice best = { true, 1, 1, 2, 1 };
+    double best_us = 1e300;
+    auto consider = [&](double us, const Choice& c) { if (us < best_us) { best_us = us; best = c; } };
+    const double stretches16 = live(16);
+    for (uint32_t nc = 1; nc <= 4; nc *= 2) {
+        const double blocks = stretches16 * (double)ceil_div(s.ctiles, nc), steps = blocks * (double)s.steps / 1024;
+        for (uint32_t splits = 1; splits <= 16; splits *= 2) {
+            if (splits > 1 && s.steps < 8 * splits) break;
+            for (uint32_t waves = 2; waves <= 8; waves *= 2) {
+                const double trips = (double)ceil_div(ceil_div(s.steps, waves * splits), 2), items = blocks * splits;
+                double us = k.call + trips * (k.trip + k.trip_nc * nc) + k.waves * std::max(0.0, items * waves / 2048 - 1) +
+                            steps * (k.steps + k.steps_nc * nc) + k.sums * items * nc / 1024;
+                if (splits > 1) us += k.split + k.split_mb * splits * out_mb;
+                consider(us, Choice{ true, 1, nc, waves, splits });
+                if (waves >= s.steps) break;
+            }
+        }
+    }
+    const double laid = direct ? 0.0 : k.t_lay + k.t_lay_mb * b * (double)s.steps * 128 * (type == HAC_TYPE_F32 ? 4 : 2) / 1e6;
+    const double fixed = k.t_call + laid + k.t_mb * out_mb * (type == HAC_TYPE_F32 ? 4 : 2);
+    if (fixed >= best_us) return best;
+    const uint64_t chunks = mode == FP4 ? s.groups : s.steps;
+    const uint32_t most_nr = mode == THREE ? 4 : 8;
+    for (uint32_t nr = 2; nr <= most_nr; nr *= 2) {
+        if (nr > 2 && B <= 8 * nr) break;
+        uint64_t rows = 16 * nr;
+        if (count == 1) { const uint64_t tiles = ceil_div(B, 16); rows = 16 * ceil_div(tiles, ceil_div(tiles, nr)); }   // (dealt evenly)
+        const double stretches = live(rows);
+        for (uint32_t nc = 1; nc <= 4; nc *= 2) {
+            const double blocks = stretches * (double)ceil_div(s.ctiles, 4 * nc);
+            const double mm = (mode == THREE ? 12.0 : 4.0) * (double)(rows / 16) * nc / 100;
+            for (uint32_t splits = 1; splits <= 16; splits *= 2) {
+                if (splits > chunks) break;
+                const uint64_t per = ceil_div(chunks, splits), parts = ceil_div(chunks, per);
+                const double cu = std::max(1.0, blocks * (double)parts / 256);
+                double us = fixed + (double)per * (k.t_chunk + k.t_chunk_mm * mm + cu * (k.t_cu_chunk + k.t_cu_mm * mm));
+                if (parts > 1) us += k.t_split + k.t_split_mb * (double)parts * out_mb;
+                consider(us, Choice{ false, nr, nc, 4, splits });
+            }
+        }
+    }
+    return best;
+}
+
+// whole: rows of X consist of whole, aligned pieces of 16 bytes.  bytes is what a call needs wherever X lies.
+Plan plan_mx(const hac_desc_t& d, uint32_t type, uint64_t B, uint32_t flags, bool grouped, bool whole)
 {
     const MxShape s = mx_shape(d.n, d.m);
     const uint64_t count = grouped ? d.k_sym : 1;
     Plan p = {};
     p.mode = flags & HAC_MX_QUANTIZE_X ? FP4 : type == HAC_TYPE_F32 ? THREE : ONE;
-    const uint64_t used = std::min(count, B), per = (B + used - 1) / used;           // rows a group has on average
-    p.rows = per <= 32;
-    if (p.rows) {
-        p.nr = per <= 16 ? 1 : 2;
-        p.stretches = fill(B, count, 16 * p.nr);
-        p.nc = 1;
-        p.col_blocks = s.ctiles;
-        p.waves = (uint32_t)std::min<uint64_t>(8, s.steps);
-        return p;
-    }
-    p.nr = p.mode == THREE ? 4 : per <= 64 ? 4 : 8;
-    p.nc = s.ctiles <= 4 ? 1 : s.ctiles <= 8 ? 2 : 4;
-    p.stretches = fill(B, count, 16 * p.nr);
-    p.col_blocks = (s.ctiles + 4 * p.nc - 1) / (4 * p.nc);
-    p.tiles = fill(B, count, 16);
-    const uint64_t chunks = p.mode == FP4 ? s.groups : s.steps;
-    const uint64_t blocks = (B + 16 * p.nr - 1) / (16 * p.nr) * p.col_blocks;
-    uint64_t splits = std::max<uint64_t>(1, std::min<uint64_t>(std::min<uint64_t>(512 / std::max<uint64_t>(blocks, 1), chunks / 2), 16));
-    p.per_split = (uint32_t)((chunks + splits - 1) / splits);
-    p.splits = (uint32_t)((chunks + p.per_split - 1) / p.per_split);
+    const bool pieces = p.mode == ONE && d.n % 8 == 0;
+    p.c = choose(s, B, count, d.m, type, p.mode, pieces);
     auto up = [](uint64_t v) { return (size_t)((v + 255) / 256 * 256); };
-    p.xt_bytes = up(p.mode == FP4 ? p.tiles * s.groups * 4096 : p.tiles * s.steps * step_bytes(p.mode));
-    p.xs_bytes = p.mode == FP4 ? up(p.tiles * s.groups * 256) : 0;
-    p.part_bytes = p.splits > 1 ? up((uint64_t)p.splits * B * d.m * sizeof(float)) : 0;
+    if (p.c.rows) {
+        p.rows_each = 16;
+        p.col_blocks = ceil_div(s.ctiles, p.c.nc);
+    } else {
+        p.direct = pieces && whole;
+        p.rows_each = 16 * p.c.nr;
+        if (!grouped) { const uint64_t tiles = ceil_div(B, 16); p.rows_each = 16 * (uint32_t)ceil_div(tiles, ceil_div(tiles, p.c.nr)); }
+        p.col_blocks = ceil_div(s.ctiles, 4 * p.c.nc);
+        p.tiles = fill(B, count, 16);
+        const uint64_t chunks = p.mode == FP4 ? s.groups : s.steps;
+        p.per_split = (uint32_t)ceil_div(chunks, p.c.splits);
+        p.c.splits = (uint32_t)ceil_div(chunks, p.per_split);
+        p.xt_bytes = up(p.mode == FP4 ? p.tiles * s.groups * 4096 : p.tiles * s.steps * step_bytes(p.mode));
+        p.xs_bytes = p.mode == FP4 ? up(p.tiles * s.groups * 256) : 0;
+    }
+    p.stretches = fill(B, count, p.rows_each);
+    p.part_bytes = p.c.splits > 1 ? up((uint64_t)p.c.splits * B * d.m * sizeof(float)) : 0;
     p.bytes = p.xt_bytes + p.xs_bytes + p.part_bytes;
     return p;
 }
 
-template <int MODE, typename T, int NR, int NC>
-int launch_rows(const Plan& p, const MxW& w, const T* X, uint64_t ldx, uint32_t B, const int32_t* offsets, T* Y, uint64_t ldy, hipStream_t stream)
+template <int MODE, typename T, int NC>
+int launch_rows(const Plan& p, const MxW& w, const T* X, uint64_t ldx, uint32_t B, const int32_t* offsets, T* Y, uint64_t ldy, float* part,
+                hipStream_t stream)
 {
-    constexpr int U = MODE == THREE ? 2 : 4;
-    hipLaunchKernelGGL((mx_rows_kernel<MODE, T, NR, NC, U>), dim3((uint32_t)(p.stretches * p.col_blocks)), dim3(64 * p.waves),
-                       (size_t)p.waves * NR * NC * 1024, stream, w, X, ldx, B, offsets, Y, ldy, (uint32_t)p.col_blocks);
-    note_kernel("mx_rows_kernel<%d, %s, %d, %d, %d>", MODE, type_name(X), NR, NC, U);
+    constexpr int U = 2;
+    hipLaunchKernelGGL((mx_rows_kernel<MODE, T, NC, U>), dim3((uint32_t)p.col_blocks, (uint32_t)p.stretches, p.c.splits), dim3(64 * p.c.waves),
+                       (size_t)p.c.waves * NC * 1024, stream, w, X, ldx, B, offsets, Y, ldy, w.steps / (p.c.splits * p.c.waves), w.steps % (p.c.splits * p.c.waves), part);
+    note_kernel("mx_rows_kernel<%d, %s, %d, %d>", MODE, type_name(X), NC, U);
     return launched();
 }
 
-template <int MODE, typename T, int NR, int NC>
-int launch_tile(const Plan& p, const MxW& w, const uint8_t* xt, const uint8_t* xs, uint32_t B, const int32_t* offsets, T* Y, uint64_t ldy,
-                float* part, hipStream_t stream)
+struct Operands {                                // of a product on tiles: X laid out, or X itself (ldx), and where partial sums go
+    const uint8_t *xt, *xs;
+    uint64_t ldx;
+    float* part;
+};
+
+template <int MODE, bool DIRECT, typename T, int NR, int NC>
+int launch_tile(const Plan& p, const MxW& w, const Operands& x, uint32_t B, const int32_t* offsets, T* Y, uint64_t ldy, hipStream_t stream)
 {
-    auto k = mx_tile_kernel<MODE, T, NR, NC>;
+    auto k = mx_tile_kernel<MODE, DIRECT, T, NR, NC>;
     constexpr size_t lds = 2 * NR * chunk_bytes<MODE>();
     if (lds > 64 * 1024) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         if (e != hipSuccess) return hip_fail(e);
     }
-    const uint64_t items = p.stretches * p.col_blocks * p.splits;
-    hipLaunchKernelGGL(k, dim3((uint32_t)((items + 7) / 8 * 8)), dim3(256), lds, stream, w, xt, xs, (uint32_t)p.tiles, B, offsets, Y, ldy,
-                       (uint32_t)p.stretches, (uint32_t)p.col_blocks, p.splits, p.per_split, part);
-    note_kernel("mx_tile_kernel<%d, %s, %d, %d>", MODE, type_name(Y), NR, NC);
+    const uint64_t items = p.stretches * p.col_blocks * p.c.splits;
+    hipLaunchKernelGGL(k, dim3((uint32_t)((items + 7) / 8 * 8)), dim3(256), lds, stream, w, x.xt, x.xs, x.ldx, (uint32_t)p.tiles, B, offsets, Y, ldy,
+                       p.rows_each, (uint32_t)p.stretches, (uint32_t)p.col_blocks, p.c.splits, p.per_split, x.part);
+    note_kernel("mx_tile_kernel<%d, %s, %s, %d, %d>", MODE, DIRECT ? "true" : "false", type_name(Y), NR, NC);
     return launched();
+}
+
+template <int MODE, bool DIRECT, typename T>
+int pick_tile(const Plan& p, const MxW& w, const Operands& x, uint32_t B, const int32_t* offsets, T* Y, uint64_t ldy, hipStream_t stream)
+{
+    auto columns = [&](auto rows) {
+        constexpr int NR = decltype(rows)::value;
+        return p.c.nc == 1 ? launch_tile<MODE, DIRECT, T, NR, 1>(p, w, x, B, offsets, Y, ldy, stream)
+             : p.c.nc == 2 ? launch_tile<MODE, DIRECT, T, NR, 2>(p, w, x, B, offsets, Y, ldy, stream)
+                           : launch_tile<MODE, DIRECT, T, NR, 4>(p, w, x, B, offsets, Y, ldy, stream);
+    };
+    if (p.c.nr == 2) return columns(std::integral_constant<int, 2>{});
+    if (p.c.nr == 4) return columns(std::integral_constant<int, 4>{});
+    return columns(std::integral_constant<int, MODE == THREE ? 4 : 8>{});
 }
 
 template <int MODE, typename T>
 int run_mode(const Plan& p, const MxW& w, const T* X, uint64_t ldx, uint32_t B, const int32_t* offsets, T* Y, uint64_t ldy, uint8_t* ws,
              hipStream_t stream)
 {
-    if (p.rows) {
-        if (p.nr == 1) return launch_rows<MODE, T, 1, 1>(p, w, X, ldx, B, offsets, Y, ldy, stream);
-        return launch_rows<MODE, T, 2, 1>(p, w, X, ldx, B, offsets, Y, ldy, stream);
-    }
-    uint8_t* xt = ws;
-    uint8_t* xs = ws + p.xt_bytes;
-    float* part = reinterpret_cast<float*>(ws + p.xt_bytes + p.xs_bytes);
-    hipLaunchKernelGGL((mx_lay_out_kernel<MODE, T>), dim3((uint32_t)p.tiles, w.groups), dim3(256), 0, stream, X, ldx, w.n, w.steps, w.groups, B,
-                       offsets, w.count, xt, xs);
-    note_kernel("mx_lay_out_kernel<%d, %s>", MODE, type_name(X));
-    int rc = launched();
-    if (rc) return rc;
-    constexpr int MOST = MODE == THREE ? 4 : 8;
-    if (p.nr == MOST) {
-        rc = p.nc == 1 ? launch_tile<MODE, T, MOST, 1>(p, w, xt, xs, B, offsets, Y, ldy, part, stream)
-           : p.nc == 2 ? launch_tile<MODE, T, MOST, 2>(p, w, xt, xs, B, offsets, Y, ldy, part, stream)
-                       : launch_tile<MODE, T, MOST, 4>(p, w, xt, xs, B, offsets, Y, ldy, part, stream);
+    const Operands x = { p.direct ? reinterpret_cast<const uint8_t*>(X) : ws, ws + p.xt_bytes, ldx,
+                         reinterpret_cast<float*>(ws + p.xt_bytes + p.xs_bytes) };
+    int rc = HAC_OK;
+    if (p.c.rows) {
+        rc = p.c.nc == 1 ? launch_rows<MODE, T, 1>(p, w, X, ldx, B, offsets, Y, ldy, x.part, stream)
+           : p.c.nc == 2 ? launch_rows<MODE, T, 2>(p, w, X, ldx, B, offsets, Y, ldy, x.part, stream)
+                       : launch_rows<MODE, T, 4>(p, w, X, ldx, B, offsets, Y, ldy, x.part, stream);
+    } else if (p.direct) {
+        if constexpr (MODE == ONE) rc = pick_tile<MODE, true, T>(p, w, x, B, offsets, Y, ldy, stream);
     } else {
-        rc = p.nc == 1 ? launch_tile<MODE, T, 4, 1>(p, w, xt, xs, B, offsets, Y, ldy, part, stream)
-           : p.nc == 2 ? launch_tile<MODE, T, 4, 2>(p, w, xt, xs, B, offsets, Y, ldy, part, stream)
-                       : launch_tile<MODE, T, 4, 4>(p, w, xt, xs, B, offsets, Y, ldy, part, stream);
+        hipLaunchKernelGGL((mx_lay_out_kernel<MODE, T>), dim3((uint32_t)p.tiles, w.groups), dim3(256), 0, stream, X, ldx, w.n, w.steps, w.groups, B,
+                           offsets, w.count, ws, ws + p.xt_bytes);
+        note_kernel("mx_lay_out_kernel<%d, %s>", MODE, type_name(X));
+        rc = launched();
+        if (!rc) rc = pick_tile<MODE, false, T>(p, w, x, B, offsets, Y, ldy, stream);
     }
-    if (rc || p.splits == 1) return rc;
+    if (rc || p.c.splits == 1) return rc;
     const uint64_t total = (uint64_t)B * w.m;
-    hipLaunchKernelGGL(mx_sum_kernel<T>, dim3((uint32_t)std::min<uint64_t>((total + 255) / 256, 4096)), dim3(256), 0, stream, part, p.splits, B,
+    hipLaunchKernelGGL(mx_sum_kernel<T>, dim3((uint32_t)std::min<uint64_t>((total + 255) / 256, 4096)), dim3(256), 0, stream, x.part, p.c.splits, B,
                        w.m, offsets, w.count, Y, ldy);
     note_kernel("mx_sum_kernel<%s>", type_name(Y));
     return launched();
@@ -773,8 +1024,8 @@ int run_typed(const Plan& p, const MxW& w, const void* X, uint64_t ldx, uint32_t
 // a launch's grid, in threads per dimension, has 32 bits
 bool grids_fit(const Plan& p, const MxShape& s)
 {
-    if (p.rows) return p.stretches * p.col_blocks <= 0xffffffffull / (64 * p.waves);
-    return p.tiles <= 0xffffffull && s.groups <= 65535 && p.stretches <= 0xffffffull && p.stretches * p.col_blocks * p.splits <= 0xfffff0ull;
+    if (p.c.rows) return p.col_blocks <= 0xffffffffull / (64 * p.c.waves) && p.stretches <= 65535;
+    return p.tiles <= 0xffffffull && s.groups <= 65535 && p.stretches * p.col_blocks <= 0xfffff0ull / p.c.splits;
 }
 
 bool aligned(const void* p, uint32_t type) { return reinterpret_cast<uintptr_t>(p) % (type == HAC_TYPE_F32 ? 4 : 2) == 0; }
@@ -788,7 +1039,8 @@ int product(const hac_desc_t* desc, const void* d_blob, uint32_t type, const voi
     if (B == 0) return HAC_OK;
     if (!d_X || !d_Y || ldx < (int64_t)desc->n || ldy < (int64_t)desc->m || !aligned(d_X, type) || !aligned(d_Y, type)) return HAC_EINVAL;
     if (B > kMostRows) return HAC_ERANGE;
-    const Plan p = plan_mx(*desc, type, (uint64_t)B, flags, grouped);
+    const bool whole = desc->n % 8 == 0 && ldx % 8 == 0 && reinterpret_cast<uintptr_t>(d_X) % 16 == 0;
+    const Plan p = plan_mx(*desc, type, (uint64_t)B, flags, grouped, whole);
     if (!grids_fit(p, mx_shape(desc->n, desc->m))) return HAC_ERANGE;
     if (p.bytes && (!d_ws || ws_bytes < p.bytes)) return HAC_EWORKSPACE;
     if (p.bytes && reinterpret_cast<uintptr_t>(d_ws) % 256) return HAC_EINVAL;
@@ -876,7 +1128,7 @@ extern "C" size_t mx_workspace_bytes(const hac_desc_t* desc, uint32_t type, int6
 {
     if (!desc || !mx_header_ok(*desc) || type > HAC_TYPE_BF16 || (flags & ~HAC_MX_QUANTIZE_X) || B <= 0 || B > kMostRows) return 0;
     if (!grouped && desc->k_sym != 1) return 0;
-    return plan_mx(*desc, type, (uint64_t)B, flags, grouped != 0).bytes;
+    return plan_mx(*desc, type, (uint64_t)B, flags, grouped != 0, false).bytes;
 }
 
 extern "C" int mx_dot(const hac_desc_t* desc, const void* d_blob, uint32_t type, const void* d_X, int64_t B, int64_t ldx,

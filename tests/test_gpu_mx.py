@@ -206,11 +206,13 @@ def test_nan_and_infinity_in_x(hac, B, dtype):
 def test_no_rows_and_no_workspace_of_ones_own(hac):
     db = hac.mx_encode(layer(300, 40)).to_device(DEV)
     assert hac.mx_dot(db, torch.zeros((0, 300), device=DEV)).shape == (0, 40)
-    X = batch(100, 300, F32)
-    need = hac.mx_workspace_bytes(db.desc, 100)
+    w = layer(2048, 2048)
+    db, X = hac.mx_encode(w).to_device(DEV), batch(2000, 2048, F32)
+    need = hac.mx_workspace_bytes(db.desc, 2000)
+    assert need
     ws = torch.full((need + 256,), 0xff, dtype=torch.uint8, device=DEV)
     Y = hac.mx_dot(db, X.to(DEV), workspace=ws[:need])
-    check(Y, X, layer(300, 40), False, "workspace")
+    check(Y, X, w, False, "workspace")
     assert bool((ws[need:] == 0xff).all())
     with pytest.raises(hac.HacError) as e:
         hac.mx_dot(db, X.to(DEV), workspace=ws[:need - 1])

@@ -143,6 +143,7 @@ REFUSE = """
 F32, BF16, Q = 0, 1, 1
 d = hac.mx_describe(300, 40)
 many = hac.mx_describe(300, 40, 3)
+big, bigger = hac.mx_describe(4096, 4096), hac.mx_describe(4096, 4096, 2)      # 500 rows take a workspace
 broken = hac.mx_describe(300, 40); broken.off_stream += 256
 at = lambda x: C.c_void_p(x << 20)
 def dot(desc=d, blob=at(1), type=F32, X=at(2), B=4, ldx=300, Y=at(3), ldy=40, flags=0, ws=at(4), bytes=1 << 30):
@@ -160,9 +161,10 @@ for call, rc in (
     (lambda: dot(blob=C.c_void_p((1 << 20) + 16)), -1), (lambda: dot(type=2), -1), (lambda: dot(flags=2), -1), (lambda: dot(B=-1), -1),
     (lambda: dot(X=None), -1), (lambda: dot(Y=None), -1), (lambda: dot(ldx=299), -1), (lambda: dot(ldy=39), -1), (lambda: dot(X=odd), -1),
     (lambda: dot(type=BF16, X=odd), -1), (lambda: dot(Y=odd), -1), (lambda: dot(B=(1 << 27) + 1), -4),
-    (lambda: dot(B=200, ws=None), -6), (lambda: dot(B=200, bytes=16), -6), (lambda: dot(B=200, ws=C.c_void_p((4 << 20) + 16)), -1),
+    (lambda: dot(desc=big, B=500, ldx=4096, ldy=4096, ws=None), -6), (lambda: dot(desc=big, B=500, ldx=4096, ldy=4096, bytes=16), -6),
+    (lambda: dot(desc=big, B=500, ldx=4096, ldy=4096, ws=C.c_void_p((4 << 20) + 16)), -1),
     (lambda: dot(B=0, X=None, Y=None), 0),
-    (lambda: grouped(offsets=None), -1), (lambda: grouped(offsets=odd), -1), (lambda: grouped(B=600, ws=None), -6), (lambda: grouped(B=0), 0),
+    (lambda: grouped(offsets=None), -1), (lambda: grouped(offsets=odd), -1), (lambda: grouped(desc=bigger, B=600, ldx=4096, ldy=4096, ws=None), -6), (lambda: grouped(B=0), 0),
     (lambda: encode(desc=None), -1), (lambda: encode(W=None), -1), (lambda: encode(type=7), -1), (lambda: encode(ldw=39), -1),
     (lambda: encode(count=2, stride=300 * 40 - 1), -1), (lambda: encode(count=0), -1), (lambda: encode(W=odd), -1),
     (lambda: encode(blob=None), -6), (lambda: encode(room=100), -6), (lambda: encode(blob=C.c_void_p((2 << 20) + 64)), -1),
@@ -225,14 +227,14 @@ def test_refused_arguments(call, args, kw, error, text):
 
 def test_workspace_of_a_chain_with_such_a_layer():
     import ctypes
-    w1, w2 = layer(300, 64), layer(64, 40)
+    w1, w2 = layer(2048, 2048), layer(2048, 40)
     a, b = hac.mx_encode(w1), hac.hac_encode(np.where(np.abs(w2) > 1, np.float32(0.5), np.float32(0)))
     layers = (hac.Layer * 2)()
     for l, blob in zip(layers, (a, b)):
         l.desc, l.d_blob = ctypes.pointer(blob.desc), 1 << 20
     lib = hac.load_library()
-    assert lib.hac_forward_workspace_bytes(layers, 2, 100) > 0
-    assert hac.hac_workspace_bytes(a.desc, 100) == hac.mx_workspace_bytes(a.desc, 100) > 0
-    many = hac.mx_encode(layer(300, 64, count=2))
+    assert lib.hac_forward_workspace_bytes(layers, 2, 2000) > 0
+    assert hac.hac_workspace_bytes(a.desc, 2000) == hac.mx_workspace_bytes(a.desc, 2000) > 0
+    many = hac.mx_encode(layer(2048, 2048, count=2))
     layers[0].desc = ctypes.pointer(many.desc)
-    assert lib.hac_forward_workspace_bytes(layers, 2, 100) == 0                        # a layer is one matrix
+    assert lib.hac_forward_workspace_bytes(layers, 2, 2000) == 0                        # a layer is one matrix

@@ -498,22 +498,27 @@ mx_rows_kernel(MxW w, const T* __restrict__ X, uint64_t ldx, uint32_t B, const i
 }
 
 // ---- many rows -----------------------------------------------------------------------------------
-// X in operand order, group by group, each group from a tile of 16 rows of its own on, zeros behind entry n: quantised codes (and
+// X in operand order, group by group, each group from a tile of 16 rows of its own on, zeros behind entry n up to a whole group of four steps: quantised codes (and
 // their scales in groups of four tiles, as W's); bf16 rows as [tile][step][row][piece of 8 k], pieces in an order that differs from
 // row to row (turned); the three parts of fp32 rows as [tile][step][half][part][operand][lane][16 bytes].
 // (A wavefront has a tile's step, a lane a block of its row.)
-template <int MODE> __host__ __device__ constexpr uint32_t chunk_bytes()          // of 16 rows: what is staged at once
-{
-    return MODE == FP4 ? 4096u + 256u : MODE == ONE ? 4096u : 6144u;
-}
 __host__ __device__ constexpr uint32_t step_bytes(int mode) { return mode == FP4 ? 1024u : 4096u * mode; }
+// Steps of a chunk, which is what a block stages and requests at once, and chunks of a step.  Few rows are multiplied quickly: several steps
+// at once keep more of W in flight (9973 x 1511, 137 bf16 rows 24.0 -> 20.8 us), unless three parts of them leave LDS room for one block
+// a CU (25088 x 4096, 32 fp32 rows 31.9 -> 34.9).
+__host__ __device__ constexpr int chunk_steps(int mode, int nr) { return mode == FP4 ? 4 : mode == THREE ? 1 : nr <= 2 ? 4 : nr <= 4 ? 2 : 1; }
+__host__ __device__ constexpr int chunk_halves(int mode) { return mode == THREE ? 2 : 1; }
+__host__ __device__ constexpr uint32_t chunk_bytes(int mode, int nr)                 // of 16 rows
+{
+    return mode == FP4 ? 4096u + 256u : step_bytes(mode) * chunk_steps(mode, nr) / chunk_halves(mode);
+}
 // where a piece of a row lies: any 16 lanes that LDS serves at a time (0 .. 3, 12 .. 15, 20 .. 27 and so on) read from 16 different ones
 __device__ __forceinline__ uint32_t turned(uint32_t row, uint32_t piece) { return piece ^ ((row & 3) | ((0u - row / 4) & 3) << 2); }
 __device__ __forceinline__ uint32_t place(uint32_t row, uint32_t piece) { return row * 256 + turned(row, piece) * 16; }
 
 template <int MODE, typename T>
 __global__ void __launch_bounds__(256)
-mx_lay_out_kernel(const T* __restrict__ X, uint64_t ldx, uint32_t n, uint32_t steps, uint32_t groups, uint32_t B,
+mx_lay_out_kernel(const T* __restrict__ X, uint64_t ldx, uint32_t n, uint32_t groups, uint32_t B,
                   const int32_t* __restrict__ offsets, uint32_t count, uint8_t* __restrict__ out, uint8_t* __restrict__ out_scales)
 {
     __shared__ uint8_t bytes[256];
@@ -527,7 +532,7 @@ mx_lay_out_kernel(const T* __restrict__ X, uint64_t ldx, uint32_t n, uint32_t st
     Block32<T> x;
     if (step * 128 + 128 <= n) x.load_step(row + step * 128, g, words);
     else x.load_step(row + step * 128, g, words, n > step * 128 ? n - step * 128 : 0u, n);
-    if constexpr (MODE == FP4) {                             // steps: 4 * groups
+    if constexpr (MODE == FP4) {
         uint32_t byte;
         const u32x4 q = quantise(x, byte);
         *reinterpret_cast<u32x4*>(out + (((uint64_t)tile * groups * 4 + step) * 64 + lane) * 16) = q;
@@ -536,8 +541,7 @@ mx_lay_out_kernel(const T* __restrict__ X, uint64_t ldx, uint32_t n, uint32_t st
         if (threadIdx.x < 64)
             reinterpret_cast<uint32_t*>(out_scales)[((uint64_t)tile * groups + blockIdx.y) * 64 + lane] = reinterpret_cast<const uint32_t*>(bytes)[lane];
     } else {
-        if (step >= steps) return;
-        uint8_t* to = out + ((uint64_t)tile * steps + step) * step_bytes(MODE);
+        uint8_t* to = out + ((uint64_t)tile * groups * 4 + step) * step_bytes(MODE);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             u32x4 p[MODE];
@@ -588,8 +592,8 @@ mx_tile_kernel(MxW w, const uint8_t* __restrict__ xt, const uint8_t* __restrict_
                const int32_t* __restrict__ offsets, T* __restrict__ Y, uint64_t ldy, uint32_t rows_each, uint32_t stretches,
                uint32_t col_blocks, uint32_t splits, uint32_t per_split, float* __restrict__ part)
 {
-    constexpr uint32_t CH = chunk_bytes<MODE>(), STAGE = NR * CH;
-    constexpr int HALVES = MODE == THREE ? 2 : 1, WS = MODE == FP4 ? 4 : 1;      // chunks of a step; steps of a chunk
+    constexpr uint32_t CH = chunk_bytes(MODE, NR), STAGE = NR * CH;
+    constexpr int CS = chunk_steps(MODE, NR), HALVES = chunk_halves(MODE);
     extern __shared__ __align__(16) uint8_t lds[];               // two stages
     const uint32_t lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
     // consecutive items on one XCD; the stretches of a column block follow one another and share its part of W in that L2
@@ -600,7 +604,7 @@ mx_tile_kernel(MxW w, const uint8_t* __restrict__ xt, const uint8_t* __restrict_
     const Item it = find_item(offsets, w.count, B, rows_each, stretch);
     const uint32_t tiles = (it.rows + 15) / 16;
     if (!it.rows || (!DIRECT && it.tile + tiles > max_tiles)) return;
-    const uint32_t chunks = MODE == FP4 ? w.groups : w.steps;    // (a step, or a group of four)
+    const uint32_t chunks = (w.steps + CS - 1) / CS;
     const uint32_t c0 = split * per_split, c1 = min(chunks, c0 + per_split);
 
     const uint8_t* code[NC];
@@ -622,19 +626,23 @@ mx_tile_kernel(MxW w, const uint8_t* __restrict__ xt, const uint8_t* __restrict_
     auto stage = [&](auto count, uint32_t ch, uint32_t half, uint8_t* to) ALWAYS_INLINE {
         constexpr uint32_t N = decltype(count)::value;
         if constexpr (DIRECT) {
-            const bool inside = ch * 128 + 8 * piece < w.n;
 #pragma unroll
-            for (uint32_t t = 0; t < N; ++t) {
-                const uint8_t* from = (t + 1 < tiles ? first + t * (32 * ldx) : end) + (uint64_t)ch * 256;
-                to_lds(inside ? from : reinterpret_cast<const uint8_t*>(zeros16), to + t * 4096 + wave * 1024);
+            for (int c = 0; c < CS; ++c) {
+                const uint32_t step = ch * CS + c;
+                const bool inside = step * 128 + 8 * piece < w.n;
+#pragma unroll
+                for (uint32_t t = 0; t < N; ++t) {
+                    const uint8_t* from = (t + 1 < tiles ? first + t * (32 * ldx) : end) + (uint64_t)step * 256;
+                    to_lds(inside ? from : reinterpret_cast<const uint8_t*>(zeros16), to + t * CH + c * 4096 + wave * 1024);
+                }
             }
         } else {
-            constexpr uint32_t PIECES = (MODE == FP4 ? 4096u : CH) / 1024;
+            constexpr uint32_t PIECES = CH / 1024;               // (the scales' 256 bytes apart)
 #pragma unroll
             for (uint32_t i = 0; i < (N * PIECES + 3) / 4; ++i) {
                 const uint32_t z = wave + 4 * i, t = z / PIECES, p = z - t * PIECES;
                 if (N * PIECES % 4 && z >= N * PIECES) break;
-                const uint64_t at = ((uint64_t)(it.tile + min(t, tiles - 1)) * chunks + ch) * (MODE == FP4 ? 4096 : step_bytes(MODE)) + half * CH;
+                const uint64_t at = ((uint64_t)(it.tile + min(t, tiles - 1)) * w.groups * 4 + ch * CS) * step_bytes(MODE) + half * CH;
                 to_lds(xt + at + p * 1024, lane16, to + t * (PIECES * 1024) + p * 1024);
             }
             if constexpr (MODE == FP4)
@@ -651,34 +659,35 @@ mx_tile_kernel(MxW w, const uint8_t* __restrict__ xt, const uint8_t* __restrict_
 #pragma unroll
     for (int j = 0; j < 4; ++j) at_lane[j] = MODE == ONE ? place(lane & 15, 4 * (lane >> 4) + j) : lane16;
 
-    // steps s of chunk ch (behind the last step: any tile, X's codes are 0 there and W's scales too)
+    // step s of chunk ch (behind the last one: any tile, X is 0 there and W's scales too)
     auto load_codes = [&](uint32_t ch, int s, u32x4 (&to)[NC]) ALWAYS_INLINE {
-        const uint32_t step = MODE == FP4 ? min(ch * 4 + s, w.steps - 1) : ch;
+        const uint32_t step = min(ch * CS + s, w.steps - 1);
 #pragma unroll
         for (int q = 0; q < NC; ++q) to[q] = *reinterpret_cast<const u32x4*>(code[q] + (uint64_t)step * 1024 + lane16);
     };
+    // the scales of chunk ch, its first step's in the lowest byte
     auto load_scales = [&](uint32_t ch, uint32_t* to) ALWAYS_INLINE {
 #pragma unroll
         for (int q = 0; q < NC; ++q) {
-            if constexpr (MODE == FP4) to[q] = *reinterpret_cast<const uint32_t*>(scale[q] + (uint64_t)ch * 256 + lane4);
-            else to[q] = *(scale[q] + (uint64_t)(ch / 4) * 256 + ch % 4 + lane4);
+            if constexpr (CS == 1) to[q] = *(scale[q] + (uint64_t)(ch / 4) * 256 + ch % 4 + lane4);
+            else to[q] = *reinterpret_cast<const uint32_t*>(scale[q] + (uint64_t)(ch * CS / 4) * 256 + lane4) >> (CS == 2 ? 16 * (ch & 1) : 0);
         }
     };
 
     // the chunks with the first N of the NR tiles of rows
     auto walk = [&](auto count) ALWAYS_INLINE {
         constexpr int N = decltype(count)::value;
-        u32x4 cur[WS][NC], next[NC];
+        u32x4 cur[CS][NC], next[MODE == FP4 ? 1 : CS][NC];
         uint32_t cur_s[NC], next_s[NC];
         bf16x8 v[2][NC];                                         // W's operand of these 32 k and the next
         const uint32_t last = (c1 - c0) * HALVES - 1;            // chunk u: step c0 + u / HALVES, half u % HALVES
         stage(count, c0, 0, lds);
         load_scales(c0, cur_s);
 #pragma unroll
-        for (int s = 0; s < WS; ++s) load_codes(c0, s, cur[s]);
+        for (int s = 0; s < CS; ++s) load_codes(c0, s, cur[s]);
         if constexpr (MODE != FP4) {
 #pragma unroll
-            for (int q = 0; q < NC; ++q) v[0][q] = weights(cur[0][q][0], scale_of(cur_s[q]));
+            for (int q = 0; q < NC; ++q) v[0][q] = weights(cur[0][q][0], scale_of(cur_s[q] & 255));
         }
         loads_done();
         uint32_t u = 0;
@@ -690,18 +699,20 @@ mx_tile_kernel(MxW w, const uint8_t* __restrict__ xt, const uint8_t* __restrict_
                 block_sync_lds();                                // all have their part of this chunk, and have read the one before
                 if (half == 0) {
                     load_scales(ahead, next_s);
-                    if constexpr (MODE != FP4) load_codes(ahead, 0, next);
+                    if constexpr (MODE != FP4)
+#pragma unroll
+                        for (int s = 0; s < CS; ++s) load_codes(ahead, s, next[s]);
                 }
                 if (u < last) stage(count, c0 + (u + 1) / HALVES, (u + 1) % HALVES, lds + (~u & 1) * STAGE);
                 ++u;
                 __builtin_amdgcn_sched_barrier(0);
                 // beat b multiplies one operand of X; what it is depends on b alone
-                constexpr int PARTS = MODE == THREE ? 3 : 1, JS = 4 / HALVES, PER = N * PARTS, BEATS = JS * PER;
+                constexpr int PARTS = MODE == THREE ? 3 : 1, JS = MODE == FP4 ? 4 : 4 * CS / HALVES, PER = N * PARTS, BEATS = JS * PER;
                 auto operand_at = [&](int b) ALWAYS_INLINE -> u32x4 {
                     const int j = b / PER, i = PARTS - 1 - b % PER / N, r = b % N;
                     if constexpr (MODE == FP4) return *reinterpret_cast<const u32x4*>(x + r * 4096 + j * 1024 + at_lane[0]);
-                    else if constexpr (MODE == ONE) return *reinterpret_cast<const u32x4*>(x + r * 4096 + at_lane[j]);
-                    else return *reinterpret_cast<const u32x4*>(x + r * CH + (i * 2 + j) * 1024 + at_lane[0]);
+                    else if constexpr (MODE == ONE) return *reinterpret_cast<const u32x4*>(x + r * CH + j / 4 * 4096 + at_lane[j % 4]);
+                    else return *reinterpret_cast<const u32x4*>(x + r * CH + (j / 2 * 6 + i * 2 + j % 2) * 1024 + at_lane[0]);
                 };
                 u32x4 xq[3];
                 uint32_t sx[N];
@@ -724,12 +735,13 @@ mx_tile_kernel(MxW w, const uint8_t* __restrict__ xt, const uint8_t* __restrict_
                             if (j == 3) acc[r][q] = multiply_fp4<3>(cur[3][q], cur_s[q], xq[b % 3], sx[r], acc[r][q]);
                         }
                     } else {
-                        const int jj = half * JS + j;            // of the step's four
+                        const int jj = half * JS + j;            // 32 k of the chunk
 #pragma unroll
                         for (int q = 0; q < NC; ++q) acc[r][q] = multiply_bf16(v[jj & 1][q], xq[b % 3], acc[r][q]);
 #pragma unroll
                         for (int q = t * NC / PER; q < (t + 1) * NC / PER; ++q)
-                            v[(jj & 1) ^ 1][q] = jj < 3 ? weights(cur[0][q][(jj + 1) & 3], scale_of(cur_s[q])) : weights(next[q][0], scale_of(next_s[q]));
+                            v[(jj & 1) ^ 1][q] = jj + 1 < 4 * CS ? weights(cur[(jj + 1) / 4 % CS][q][(jj + 1) % 4], scale_of(cur_s[q] >> 8 * ((jj + 1) / 4) & 255))
+                                                               : weights(next[0][q][0], scale_of(next_s[q] & 255));
                     }
                     __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
 #pragma unroll
@@ -749,7 +761,9 @@ mx_tile_kernel(MxW w, const uint8_t* __restrict__ xt, const uint8_t* __restrict_
 #pragma unroll
             for (int q = 0; q < NC; ++q) {
                 cur_s[q] = next_s[q];
-                if constexpr (MODE != FP4) cur[0][q] = next[q];
+                if constexpr (MODE != FP4)
+#pragma unroll
+                    for (int s = 0; s < CS; ++s) cur[s][q] = next[s][q];
             }
         }
     };
@@ -775,28 +789,36 @@ mx_tile_kernel(MxW w, const uint8_t* __restrict__ xt, const uint8_t* __restrict_
     }
 }
 
-// Y = part[0] + part[1] + ... in that order, for the rows that some group holds.
-template <typename T>
+// Y = part[0] + part[1] + ... in that order, for the rows that some group holds.  A thread has four neighbouring sums where columns come in fours
+// (V = f32x4), so that all splits' are in flight.
+template <typename T, typename V>
 __global__ void __launch_bounds__(256)
 mx_sum_kernel(const float* __restrict__ part, uint32_t splits, uint32_t B, uint32_t m, const int32_t* __restrict__ offsets, uint32_t count,
               T* __restrict__ Y, uint64_t ldy)
 {
-    uint64_t lo = 0, hi = B;
+    constexpr uint32_t E = sizeof(V) / 4;
+    uint32_t lo = 0, hi = B;
     if (offsets) {
-        lo = (uint64_t)min(max(offsets[0], 0), (int32_t)B);
-        hi = (uint64_t)min(max(offsets[count], 0), (int32_t)B);
+        lo = (uint32_t)min(max(offsets[0], 0), (int32_t)B);
+        hi = (uint32_t)min(max(offsets[count], 0), (int32_t)B);
     }
-    const uint64_t total = (uint64_t)B * m, stride = (uint64_t)gridDim.x * blockDim.x;
-    for (uint64_t i = lo * m + (uint64_t)blockIdx.x * blockDim.x + threadIdx.x; i < hi * m; i += stride) {
-        float v = part[i];
+    const uint32_t col = (blockIdx.x * 256 + threadIdx.x) * E;
+    if (col >= m) return;
+    const bool wide = (reinterpret_cast<uintptr_t>(Y) | ldy * sizeof(T)) % (4 * sizeof(T)) == 0;
+    const uint64_t next = (uint64_t)B * m;
+    for (uint32_t row = lo + blockIdx.y; row < hi; row += gridDim.y) {
+        const float* p = part + (uint64_t)row * m + col;
+        V v = *reinterpret_cast<const V*>(p);
         uint32_t s = 1;
         for (; s + 3 < splits; s += 4) {
-            const float a = part[s * total + i], b = part[(s + 1) * total + i], c = part[(s + 2) * total + i], d = part[(s + 3) * total + i];
+            const V a = *reinterpret_cast<const V*>(p + s * next), b = *reinterpret_cast<const V*>(p + (s + 1) * next);
+            const V c = *reinterpret_cast<const V*>(p + (s + 2) * next), d = *reinterpret_cast<const V*>(p + (s + 3) * next);
             v += a; v += b; v += c; v += d;
         }
-        for (; s < splits; ++s) v += part[s * total + i];
-        const uint64_t row = i / m;
-        Y[row * ldy + (i - row * m)] = (T)v;
+        for (; s < splits; ++s) v += *reinterpret_cast<const V*>(p + s * next);
+        T* y = Y + (uint64_t)row * ldy;
+        if constexpr (E == 4) store4(y, col, m, wide, v);
+        else y[col] = (T)v;
     }
 }
 
@@ -822,6 +844,8 @@ constexpr int64_t kMostRows = 1 << 27;
 // columns.  splits: parts that the k of a column are cut into.
 struct Choice { bool rows; uint32_t nr, nc, waves, splits; };
 
+constexpr uint32_t most_nc(int mode, uint32_t nr) { return mode == ONE && nr == 8 ? 2 : 4; }       // (more sums and operands than registers)
+
 struct Plan {
     Choice c;
     bool direct;                                 // tiles of X as it lies
@@ -834,22 +858,23 @@ struct Plan {
 uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 uint64_t fill(uint64_t B, uint64_t count, uint64_t R) { return std::min<uint64_t>(B, (B + (R - 1) * count) / R); }
 
-// The split with the shortest estimate of a call's time.  Its form and constants (us) were fitted to the measured times of all splits of 260 products
-// drawn over n 64 .. 25088, m 10 .. 8192, 1 .. 12544 rows, 1 .. 64 groups: estimates are off by 10 to 19 % in the mean, and the splits they choose are
-// 2.6 % slower in the mean than the best measured ones (worst 1.35 times; the better of one split per kernel chosen by sizes alone: 45 % slower).
-//   few rows: a launch, trips to memory (two steps at a time) and what a trip grows by with each tile of columns, wavefronts beyond eight on a CU, steps
-//     of X turned into operands and steps of W multiplied per SIMD, sums stored, the pass that adds the splits and its bytes
-//   tiles: a launch, X laid out and its bytes, chunks of a block, their matrix instructions, both times the blocks of a CU, the blocks, the
-//     pass that adds the splits and its bytes, Y
+// The split with the shortest estimate of a call's time.  Its form and constants (us) were fitted to the measured times of all splits of 600 products
+// drawn over n 64 .. 25088, m 10 .. 8192, 1 .. 12544 rows, 1 .. 64 groups: estimates are off by 9 to 20 % in the mean, and the splits they choose are
+// 3.3 % slower in the mean than the best measured ones (six of 600 more than a third; the better of one split per kernel chosen by sizes alone: 45 %).
+//   few rows: a launch; trips to memory, two steps each, and what a trip grows by with each tile of columns; wavefronts beyond eight on a CU;
+//     steps of X turned into operands and of W multiplied per SIMD, and those that a SIMD has more where blocks are fewer than CUs; sums stored;
+//     the pass that adds the splits and its megabytes
+//   tiles: a launch; X laid out and its megabytes; chunks of a block and their matrix instructions, both also times the blocks of a CU; the blocks of
+//     a CU; the pass that adds the splits and its megabytes; Y's
 struct Costs {
-    double call, trip, trip_nc, waves, steps, steps_nc, sums, split, split_mb;
-    double t_call, t_lay, t_lay_mb, t_chunk, t_chunk_mm, t_cu_chunk, t_cu_mm, t_split, t_split_mb, t_mb;
+    double call, trip, trip_nc, waves, steps, steps_nc, alone, sums, split, split_mb;
+    double t_call, t_lay, t_lay_mb, t_chunk, t_chunk_mm, t_cu_chunk, t_cu_mm, t_cu, t_split, t_split_mb, t_mb;
 };
 const Costs kCosts[4] = {
-    { 4.08, 0.85, 0.06, 0.70, 0.52, 0.147, 0.06, 1.8, 6.5, 0.0, 8.02, 0.203, 0.238, 0.000, 0.053, 1.546, 1.50, 3.25, 0.61 },    // codes, from fp32
-    { 3.54, 0.84, 0.11, 0.66, 0.32, 0.080, 0.27, 2.8, 2.1, 0.0, 7.59, 0.259, 0.000, 0.557, 0.171, 1.217, 2.46, 1.69, 0.82 },    // codes, from bf16
-    { 3.40, 1.15, 0.31, 1.09, 0.57, 0.168, 0.37, 2.8, 2.2, 0.0, 8.15, 0.487, 0.206, 0.219, 0.448, 0.620, 2.13, 2.46, 1.00 },    // fp32
-    { 3.31, 0.87, 0.16, 0.36, 0.14, 0.106, 0.00, 2.1, 10., 3.65, 3.92, 0.694, 0.249, 0.344, 0.120, 0.717, 2.10, 2.04, 1.06 },    // bf16
+    { 3.76, 0.455, 0.085, 0.485, 0.798, 0.082, 0.318, 0.300, 1.81, 3.96, 0.00, 7.82, 0.199, 0.057, 0.000, 0.112, 1.737, 0.000, 2.04, 2.19, 0.608 },   // codes, from fp32
+    { 3.44, 0.798, 0.074, 0.447, 0.292, 0.088, 0.220, 0.311, 2.27, 2.83, 0.00, 7.25, 0.257, 0.013, 0.753, 0.160, 1.123, 0.000, 2.82, 1.80, 0.744 },   // codes, from bf16
+    { 3.33, 0.858, 0.290, 0.831, 0.726, 0.148, 0.337, 0.286, 2.81, 1.39, 0.00, 7.79, 0.541, 0.217, 0.437, 0.404, 0.541, 0.000, 2.32, 2.14, 0.714 },   // fp32
+    { 3.72, 0.518, 0.159, 0.363, 0.240, 0.120, 0.160, 0.000, 1.83, 5.73, 3.84, 3.62, 0.612, 0.000, 0.787, 0.501, 0.398, 0.241, 2.22, 2.13, 1.079 },   // bf16
 };
 
 Choice choose(const MxShape& s, uint64_t B, uint64_t count, uint64_t m, uint32_t type, int mode, bool direct)
@@ -870,9 +895,11 @@ Choice choose(const MxShape& s, uint64_t B, uint64_t count, uint64_t m, uint32_t
         for (uint32_t splits = 1; splits <= 16; splits *= 2) {
             if (splits > 1 && s.steps < 8 * splits) break;
             for (uint32_t waves = 2; waves <= 8; waves *= 2) {
-                const double trips = (double)ceil_div(ceil_div(s.steps, waves * splits), 2), items = blocks * splits;
+                const uint64_t each = ceil_div(s.steps, waves * splits);
+                const double trips = (double)ceil_div(each, 2), items = blocks * splits;
                 double us = k.call + trips * (k.trip + k.trip_nc * nc) + k.waves * std::max(0.0, items * waves / 2048 - 1) +
-                            steps * (k.steps + k.steps_nc * nc) + k.sums * items * nc / 1024;
+                            steps * (k.steps + k.steps_nc * nc) + k.alone * std::max(0.0, waves * (double)each / 4 - steps) +
+                            k.sums * items * nc / 1024;
                 if (splits > 1) us += k.split + k.split_mb * splits * out_mb;
                 consider(us, Choice{ true, 1, nc, waves, splits });
                 if (waves >= s.steps) break;
@@ -881,22 +908,22 @@ Choice choose(const MxShape& s, uint64_t B, uint64_t count, uint64_t m, uint32_t
     }
     const double laid = direct ? 0.0 : k.t_lay + k.t_lay_mb * b * (double)s.steps * 128 * (type == HAC_TYPE_F32 ? 4 : 2) / 1e6;
     const double fixed = k.t_call + laid + k.t_mb * out_mb * (type == HAC_TYPE_F32 ? 4 : 2);
-    if (fixed >= best_us) return best;
-    const uint64_t chunks = mode == FP4 ? s.groups : s.steps;
+    if (fixed >= best_us || B <= 8 * std::min(count, B)) return best;      // (up to 8 rows a group tiles were never measured to be quicker)
     const uint32_t most_nr = mode == THREE ? 4 : 8;
     for (uint32_t nr = 2; nr <= most_nr; nr *= 2) {
         if (nr > 2 && B <= 8 * nr) break;
         uint64_t rows = 16 * nr;
         if (count == 1) { const uint64_t tiles = ceil_div(B, 16); rows = 16 * ceil_div(tiles, ceil_div(tiles, nr)); }   // (dealt evenly)
+        const uint64_t chunks = ceil_div(s.steps, chunk_steps(mode, nr));
         const double stretches = live(rows);
-        for (uint32_t nc = 1; nc <= 4; nc *= 2) {
+        for (uint32_t nc = 1; nc <= most_nc(mode, nr); nc *= 2) {
             const double blocks = stretches * (double)ceil_div(s.ctiles, 4 * nc);
-            const double mm = (mode == THREE ? 12.0 : 4.0) * (double)(rows / 16) * nc / 100;
+            const double mm = (mode == FP4 ? 1.0 : mode == THREE ? 4.0 * 3 : 4.0) * chunk_steps(mode, nr) * (double)(rows / 16) * nc / 100;
             for (uint32_t splits = 1; splits <= 16; splits *= 2) {
                 if (splits > chunks) break;
                 const uint64_t per = ceil_div(chunks, splits), parts = ceil_div(chunks, per);
                 const double cu = std::max(1.0, blocks * (double)parts / 256);
-                double us = fixed + (double)per * (k.t_chunk + k.t_chunk_mm * mm + cu * (k.t_cu_chunk + k.t_cu_mm * mm));
+                double us = fixed + (double)per * (k.t_chunk + k.t_chunk_mm * mm + cu * (k.t_cu_chunk + k.t_cu_mm * mm)) + k.t_cu * cu;
                 if (parts > 1) us += k.t_split + k.t_split_mb * (double)parts * out_mb;
                 consider(us, Choice{ false, nr, nc, 4, splits });
             }
@@ -924,10 +951,10 @@ Plan plan_mx(const hac_desc_t& d, uint32_t type, uint64_t B, uint32_t flags, boo
         if (!grouped) { const uint64_t tiles = ceil_div(B, 16); p.rows_each = 16 * (uint32_t)ceil_div(tiles, ceil_div(tiles, p.c.nr)); }
         p.col_blocks = ceil_div(s.ctiles, 4 * p.c.nc);
         p.tiles = fill(B, count, 16);
-        const uint64_t chunks = p.mode == FP4 ? s.groups : s.steps;
+        const uint64_t chunks = ceil_div(s.steps, chunk_steps(p.mode, p.c.nr));
         p.per_split = (uint32_t)ceil_div(chunks, p.c.splits);
         p.c.splits = (uint32_t)ceil_div(chunks, p.per_split);
-        p.xt_bytes = up(p.mode == FP4 ? p.tiles * s.groups * 4096 : p.tiles * s.steps * step_bytes(p.mode));
+        p.xt_bytes = up(p.tiles * s.groups * 4 * step_bytes(p.mode));
         p.xs_bytes = p.mode == FP4 ? up(p.tiles * s.groups * 256) : 0;
     }
     p.stretches = fill(B, count, p.rows_each);
@@ -957,7 +984,7 @@ template <int MODE, bool DIRECT, typename T, int NR, int NC>
 int launch_tile(const Plan& p, const MxW& w, const Operands& x, uint32_t B, const int32_t* offsets, T* Y, uint64_t ldy, hipStream_t stream)
 {
     auto k = mx_tile_kernel<MODE, DIRECT, T, NR, NC>;
-    constexpr size_t lds = 2 * NR * chunk_bytes<MODE>();
+    constexpr size_t lds = 2 * NR * chunk_bytes(MODE, NR);
     if (lds > 64 * 1024) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         if (e != hipSuccess) return hip_fail(e);
@@ -974,9 +1001,10 @@ int pick_tile(const Plan& p, const MxW& w, const Operands& x, uint32_t B, const 
 {
     auto columns = [&](auto rows) {
         constexpr int NR = decltype(rows)::value;
-        return p.c.nc == 1 ? launch_tile<MODE, DIRECT, T, NR, 1>(p, w, x, B, offsets, Y, ldy, stream)
-             : p.c.nc == 2 ? launch_tile<MODE, DIRECT, T, NR, 2>(p, w, x, B, offsets, Y, ldy, stream)
-                           : launch_tile<MODE, DIRECT, T, NR, 4>(p, w, x, B, offsets, Y, ldy, stream);
+        if (p.c.nc == 1) return launch_tile<MODE, DIRECT, T, NR, 1>(p, w, x, B, offsets, Y, ldy, stream);
+        if constexpr (most_nc(MODE, NR) == 4)
+            if (p.c.nc == 4) return launch_tile<MODE, DIRECT, T, NR, 4>(p, w, x, B, offsets, Y, ldy, stream);
+        return launch_tile<MODE, DIRECT, T, NR, 2>(p, w, x, B, offsets, Y, ldy, stream);
     };
     if (p.c.nr == 2) return columns(std::integral_constant<int, 2>{});
     if (p.c.nr == 4) return columns(std::integral_constant<int, 4>{});
@@ -997,17 +1025,18 @@ int run_mode(const Plan& p, const MxW& w, const T* X, uint64_t ldx, uint32_t B, 
     } else if (p.direct) {
         if constexpr (MODE == ONE) rc = pick_tile<MODE, true, T>(p, w, x, B, offsets, Y, ldy, stream);
     } else {
-        hipLaunchKernelGGL((mx_lay_out_kernel<MODE, T>), dim3((uint32_t)p.tiles, w.groups), dim3(256), 0, stream, X, ldx, w.n, w.steps, w.groups, B,
+        hipLaunchKernelGGL((mx_lay_out_kernel<MODE, T>), dim3((uint32_t)p.tiles, w.groups), dim3(256), 0, stream, X, ldx, w.n, w.groups, B,
                            offsets, w.count, ws, ws + p.xt_bytes);
         note_kernel("mx_lay_out_kernel<%d, %s>", MODE, type_name(X));
         rc = launched();
         if (!rc) rc = pick_tile<MODE, false, T>(p, w, x, B, offsets, Y, ldy, stream);
     }
     if (rc || p.c.splits == 1) return rc;
-    const uint64_t total = (uint64_t)B * w.m;
-    hipLaunchKernelGGL(mx_sum_kernel<T>, dim3((uint32_t)std::min<uint64_t>((total + 255) / 256, 4096)), dim3(256), 0, stream, x.part, p.c.splits, B,
-                       w.m, offsets, w.count, Y, ldy);
-    note_kernel("mx_sum_kernel<%s>", type_name(Y));
+    const bool fours = w.m % 4 == 0;
+    const dim3 grid((uint32_t)ceil_div(w.m, fours ? 1024 : 256), std::min(B, 16384u));
+    if (fours) hipLaunchKernelGGL((mx_sum_kernel<T, f32x4>), grid, dim3(256), 0, stream, x.part, p.c.splits, B, w.m, offsets, w.count, Y, ldy);
+    else hipLaunchKernelGGL((mx_sum_kernel<T, float>), grid, dim3(256), 0, stream, x.part, p.c.splits, B, w.m, offsets, w.count, Y, ldy);
+    note_kernel("mx_sum_kernel<%s, %s>", type_name(Y), fours ? "float __vector(4)" : "float");
     return launched();
 }
 
@@ -1022,8 +1051,9 @@ int run_typed(const Plan& p, const MxW& w, const void* X, uint64_t ldx, uint32_t
 }
 
 // a launch's grid, in threads per dimension, has 32 bits
-bool grids_fit(const Plan& p, const MxShape& s)
+bool grids_fit(const Plan& p, const MxShape& s, const hac_desc_t& d)
 {
+    if (p.c.splits > 1 && ceil_div(d.m, 256) > 0xffffffull) return false;                 // (of the pass that adds them)
     if (p.c.rows) return p.col_blocks <= 0xffffffffull / (64 * p.c.waves) && p.stretches <= 65535;
     return p.tiles <= 0xffffffull && s.groups <= 65535 && p.stretches * p.col_blocks <= 0xfffff0ull / p.c.splits;
 }
@@ -1041,7 +1071,7 @@ int product(const hac_desc_t* desc, const void* d_blob, uint32_t type, const voi
     if (B > kMostRows) return HAC_ERANGE;
     const bool whole = desc->n % 8 == 0 && ldx % 8 == 0 && reinterpret_cast<uintptr_t>(d_X) % 16 == 0;
     const Plan p = plan_mx(*desc, type, (uint64_t)B, flags, grouped, whole);
-    if (!grids_fit(p, mx_shape(desc->n, desc->m))) return HAC_ERANGE;
+    if (!grids_fit(p, mx_shape(desc->n, desc->m), *desc)) return HAC_ERANGE;
     if (p.bytes && (!d_ws || ws_bytes < p.bytes)) return HAC_EWORKSPACE;
     if (p.bytes && reinterpret_cast<uintptr_t>(d_ws) % 256) return HAC_EINVAL;
     set_last_hip_error(0);

@@ -53,6 +53,15 @@ HAC_MX_BOTH inline uint64_t mx_scale_at(const MxShape& s, uint64_t b, uint64_t j
     return ((j / 16 * s.groups + b / 16) * 64 + b % 4 * 16 + j % 16) * 4 + b / 4 % 4;
 }
 
+// Where to read the E entries that hold piece k ... k + E - 1 of a step of a row, of which the row has `left` >= 0 entries from the step's first on
+// (a row of at least E): at k, or where the row's last E begin, which may be before the step.  false: nothing is left, nothing is to be read.
+HAC_MX_BOTH inline bool mx_piece_at(uint32_t k, uint32_t left, uint32_t E, int32_t& at)
+{
+    const int32_t last = (int32_t)left - (int32_t)E;
+    at = (int32_t)k < last ? (int32_t)k : last;
+    return left != 0;
+}
+
 // The header of `count` matrices of n x m; false where they are too many or too large.
 inline bool mx_header(int64_t count, int64_t n, int64_t m, hac_desc_t& d)
 {

@@ -93,7 +93,9 @@ template <typename T> __device__ __forceinline__ u32x4 piece_of(const T* row, ui
         }
         return p;
     }
-    const int at = min((int)k, (int)left - E), d = (int)k - at;      // (at may lie before the step, never before the row)
+    int32_t at;
+    if (!mx_piece_at(k, left, E, at)) return p;
+    const int d = (int)k - at;
     p = load16(row + at, words);
     if constexpr (E == 8) {
         if (d & 1) p = u32x4{p.x >> 16 | p.y << 16, p.y >> 16 | p.z << 16, p.z >> 16 | p.w << 16, p.w >> 16};
@@ -560,7 +562,7 @@ mx_lay_out_kernel(const T* __restrict__ X, uint64_t ldx, uint32_t n, uint32_t gr
 // The order of a chunk is spelled out in beats of NC matrix instructions: left to itself the compiler reads an operand right before its
 // use and waits.  A beat's operand of X is read two beats ahead, and W's operands of the next 32 k are expanded beside this one's products.
 // DIRECT: bf16 rows whose pieces of 8 k are whole and aligned need no laying out, they are staged from where they are.
-__device__ __constant__ uint32_t zeros16[4] = {0, 0, 0, 0};
+__device__ __constant__ __attribute__((aligned(16))) uint32_t zeros16[4] = {0, 0, 0, 0};
 
 // 16 bytes (4) a lane from memory to lds + 16 (4) * lane, past the registers.  In assembly, so that the compiler counts its own loads only: with
 // these among them it waits for everything in flight wherever it needs one load or one read of LDS.  A wait for its own loads waits for these too

@@ -2,6 +2,8 @@
 import ctypes as C
 import os
 import re
+import shutil
+import subprocess
 import sys
 
 import numpy as np
@@ -238,3 +240,13 @@ def test_workspace_of_a_chain_with_such_a_layer():
     many = hac.mx_encode(layer(2048, 2048, count=2))
     layers[0].desc = ctypes.pointer(many.desc)
     assert lib.hac_forward_workspace_bytes(layers, 2, 2000) == 0                        # a layer is one matrix
+
+
+def test_reads_of_a_step_that_is_not_whole_stay_inside_the_row(tmp_path):
+    gxx = shutil.which("g++")
+    if gxx is None:
+        pytest.skip("no g++")
+    exe = str(tmp_path / "mx_reads")
+    subprocess.run([gxx, "-std=c++17", "-O1", "-o", exe, os.path.join(ROOT, "tests", "native", "mx_reads.cpp")], check=True, timeout=120)
+    run = subprocess.run([exe], capture_output=True, text=True, timeout=120)
+    assert run.returncode == 0 and " 0 failures" in run.stdout, run.stdout

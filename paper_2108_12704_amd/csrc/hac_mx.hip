@@ -860,26 +860,32 @@ struct Plan {
 uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 uint64_t fill(uint64_t B, uint64_t count, uint64_t R) { return std::min<uint64_t>(B, (B + (R - 1) * count) / R); }
 
-// The split with the shortest estimate of a call's time.  Its form and constants (us) were fitted to the measured times of all splits of 600 products
-// drawn over n 64 .. 25088, m 10 .. 8192, 1 .. 12544 rows, 1 .. 64 groups: estimates are off by 9 to 20 % in the mean, and the splits they choose are
-// 3.3 % slower in the mean than the best measured ones (six of 600 more than a third; the better of one split per kernel chosen by sizes alone: 45 %).
+// The split with the shortest estimate of a call's time.  Its form and constants (us) were fitted to the measured times of all splits of 800 products
+// drawn over n 64 .. 25088, m 10 .. 8192, 1 .. 12544 rows, 1 .. 64 groups: estimates are off by 10 to 14 % in the mean, and the splits they choose are
+// 3.0 % slower in the mean than the best measured ones, at most 1.47 times (one split per kernel, chosen by rows alone: 45 %).
 //   few rows: a launch; trips to memory, two steps each, and what a trip grows by with each tile of columns; wavefronts beyond eight on a CU;
-//     steps of X turned into operands and of W multiplied per SIMD, and those that a SIMD has more where blocks are fewer than CUs; sums stored;
-//     the pass that adds the splits and its megabytes
-//   tiles: a launch; X laid out and its megabytes; chunks of a block and their matrix instructions, both also times the blocks of a CU; the blocks of
-//     a CU; the pass that adds the splits and its megabytes; Y's
+//     steps of X turned into operands and of W multiplied per SIMD, what the former cost more where X is larger than the L2s (big) or its rows of
+//     bfloat16 have an odd length, and those that a SIMD has more where blocks are fewer than CUs; sums stored; the pass that adds the
+//     splits and its megabytes
+//   tiles: a launch; X laid out and its megabytes; chunks of a block and their matrix instructions; the blocks of a CU; a hundred steps of a
+//     block times the blocks of a CU, for 2, 4, 8 tiles of rows and 1, 2, 4 of columns a wavefront; the pass that adds the splits and its
+//     megabytes; Y's megabytes and W's
 struct Costs {
-    double call, trip, trip_nc, waves, steps, steps_nc, alone, sums, split, split_mb;
-    double t_call, t_lay, t_lay_mb, t_chunk, t_chunk_mm, t_cu_chunk, t_cu_mm, t_cu, t_split, t_split_mb, t_mb;
+    double call, trip, trip_nc, waves, steps, steps_nc, big, odd, alone, sums, split, split_mb;
+    double t_call, t_lay, t_lay_mb, t_chunk, t_chunk_mm, t_cu, t_tile[9], t_split, t_split_mb, t_mb, t_w_mb;
 };
 const Costs kCosts[4] = {
-    { 3.76, 0.455, 0.085, 0.485, 0.798, 0.082, 0.318, 0.300, 1.81, 3.96, 0.00, 7.82, 0.199, 0.057, 0.000, 0.112, 1.737, 0.000, 2.04, 2.19, 0.608 },   // codes, from fp32
-    { 3.44, 0.798, 0.074, 0.447, 0.292, 0.088, 0.220, 0.311, 2.27, 2.83, 0.00, 7.25, 0.257, 0.013, 0.753, 0.160, 1.123, 0.000, 2.82, 1.80, 0.744 },   // codes, from bf16
-    { 3.33, 0.858, 0.290, 0.831, 0.726, 0.148, 0.337, 0.286, 2.81, 1.39, 0.00, 7.79, 0.541, 0.217, 0.437, 0.404, 0.541, 0.000, 2.32, 2.14, 0.714 },   // fp32
-    { 3.72, 0.518, 0.159, 0.363, 0.240, 0.120, 0.160, 0.000, 1.83, 5.73, 3.84, 3.62, 0.612, 0.000, 0.787, 0.501, 0.398, 0.241, 2.22, 2.13, 1.079 },   // bf16
+    { 3.85, 0.456, 0.074, 0.414, 0.584, 0.081, 0.360, 0.000, 0.311, 0.435, 1.92, 4.51,                      // codes, from fp32
+      0.00, 7.60, 0.199, 0.014, 0.029, 0.000, { 6.58, 10.7, 20.4, 11.4, 16.7, 28.8, 23.0, 30.5, 58.9 }, 1.77, 2.23, 0.583, 0.122 },
+    { 3.64, 0.609, 0.082, 0.354, 0.203, 0.070, 0.269, 0.222, 0.219, 0.381, 2.19, 2.93,                      // codes, from bf16
+      0.00, 7.13, 0.246, 0.012, 0.790, 0.000, { 5.48, 8.69, 15.4, 8.84, 11.9, 17.6, 17.7, 19.2, 29.6 }, 2.63, 1.65, 0.780, 0.082 },
+    { 3.39, 0.845, 0.270, 0.793, 0.597, 0.121, 0.474, 0.000, 0.335, 0.387, 2.63, 1.73,                      // fp32
+      0.00, 8.16, 0.557, 0.249, 0.329, 0.000, { 44.8, 61.6, 84.9, 91.6, 113.0, 176.0 }, 2.11, 1.60, 0.658, 0.000 },
+    { 3.66, 0.493, 0.159, 0.392, 0.031, 0.087, 0.280, 0.424, 0.145, 0.285, 2.18, 2.77,                      // bf16
+      3.72, 3.60, 0.648, 0.196, 0.465, 0.356, { 15.8, 21.6, 36.9, 29.4, 37.8, 55.3, 54.6, 67.0 }, 2.28, 1.87, 0.957, 0.001 },
 };
 
-Choice choose(const MxShape& s, uint64_t B, uint64_t count, uint64_t m, uint32_t type, int mode, bool direct)
+Choice choose(const MxShape& s, uint64_t B, uint64_t count, uint64_t n, uint64_t m, uint32_t type, int mode, bool direct)
 {
     const Costs& k = kCosts[(mode == FP4 ? 0 : 2) + (type == HAC_TYPE_BF16 ? 1 : 0)];
     const double b = (double)B, used = count > 1 ? 0.8 * (double)std::min(count, B) : 0.0, out_mb = b * (double)m / 1e6;
@@ -891,7 +897,8 @@ Choice choose(const MxShape& s, uint64_t B, uint64_t count, uint64_t m, uint32_t
     Choice best = { true, 1, 1, 2, 1 };
     double best_us = 1e300;
     auto consider = [&](double us, const Choice& c) { if (us < best_us) { best_us = us; best = c; } };
-    const double stretches16 = live(16);
+    const double stretches16 = live(16), x_mb = b * (double)n * (type == HAC_TYPE_F32 ? 4 : 2) / 1e6;
+    const double step = k.steps + k.big * std::min(1.0, std::max(0.0, x_mb / 8 - 0.5)) + (type == HAC_TYPE_BF16 && n % 2 ? k.odd : 0.0);
     for (uint32_t nc = 1; nc <= 4; nc *= 2) {
         const double blocks = stretches16 * (double)ceil_div(s.ctiles, nc), steps = blocks * (double)s.steps / 1024;
         for (uint32_t splits = 1; splits <= 16; splits *= 2) {
@@ -900,7 +907,7 @@ Choice choose(const MxShape& s, uint64_t B, uint64_t count, uint64_t m, uint32_t
                 const uint64_t each = ceil_div(s.steps, waves * splits);
                 const double trips = (double)ceil_div(each, 2), items = blocks * splits;
                 double us = k.call + trips * (k.trip + k.trip_nc * nc) + k.waves * std::max(0.0, items * waves / 2048 - 1) +
-                            steps * (k.steps + k.steps_nc * nc) + k.alone * std::max(0.0, waves * (double)each / 4 - steps) +
+                            steps * (step + k.steps_nc * nc) + k.alone * std::max(0.0, waves * (double)each / 4 - steps) +
                             k.sums * items * nc / 1024;
                 if (splits > 1) us += k.split + k.split_mb * splits * out_mb;
                 consider(us, Choice{ true, 1, nc, waves, splits });
@@ -909,7 +916,8 @@ Choice choose(const MxShape& s, uint64_t B, uint64_t count, uint64_t m, uint32_t
         }
     }
     const double laid = direct ? 0.0 : k.t_lay + k.t_lay_mb * b * (double)s.steps * 128 * (type == HAC_TYPE_F32 ? 4 : 2) / 1e6;
-    const double fixed = k.t_call + laid + k.t_mb * out_mb * (type == HAC_TYPE_F32 ? 4 : 2);
+    const double w_mb = (count > 1 ? used : 1.0) * (double)n * (double)m / 2e6;
+    const double fixed = k.t_call + laid + k.t_mb * out_mb * (type == HAC_TYPE_F32 ? 4 : 2) + k.t_w_mb * w_mb;
     if (fixed >= best_us || B <= 8 * std::min(count, B)) return best;      // (up to 8 rows a group tiles were never measured to be quicker)
     const uint32_t most_nr = mode == THREE ? 4 : 8;
     for (uint32_t nr = 2; nr <= most_nr; nr *= 2) {
@@ -920,12 +928,13 @@ Choice choose(const MxShape& s, uint64_t B, uint64_t count, uint64_t m, uint32_t
         const double stretches = live(rows);
         for (uint32_t nc = 1; nc <= most_nc(mode, nr); nc *= 2) {
             const double blocks = stretches * (double)ceil_div(s.ctiles, 4 * nc);
+            const double step_us = k.t_tile[(nr / 4) * 3 + nc / 2] / 100 * chunk_steps(mode, nr) * (0.2 + 0.8 * (double)rows / (16 * nr));
             const double mm = (mode == FP4 ? 1.0 : mode == THREE ? 4.0 * 3 : 4.0) * chunk_steps(mode, nr) * (double)(rows / 16) * nc / 100;
             for (uint32_t splits = 1; splits <= 16; splits *= 2) {
                 if (splits > chunks) break;
                 const uint64_t per = ceil_div(chunks, splits), parts = ceil_div(chunks, per);
                 const double cu = std::max(1.0, blocks * (double)parts / 256);
-                double us = fixed + (double)per * (k.t_chunk + k.t_chunk_mm * mm + cu * (k.t_cu_chunk + k.t_cu_mm * mm)) + k.t_cu * cu;
+                double us = fixed + (double)per * (k.t_chunk + k.t_chunk_mm * mm + cu * step_us) + k.t_cu * cu;
                 if (parts > 1) us += k.t_split + k.t_split_mb * (double)parts * out_mb;
                 consider(us, Choice{ false, nr, nc, 4, splits });
             }
@@ -942,7 +951,7 @@ Plan plan_mx(const hac_desc_t& d, uint32_t type, uint64_t B, uint32_t flags, boo
     Plan p = {};
     p.mode = flags & HAC_MX_QUANTIZE_X ? FP4 : type == HAC_TYPE_F32 ? THREE : ONE;
     const bool pieces = p.mode == ONE && d.n % 8 == 0;
-    p.c = choose(s, B, count, d.m, type, p.mode, pieces);
+    p.c = choose(s, B, count, d.n, d.m, type, p.mode, pieces);
     auto up = [](uint64_t v) { return (size_t)((v + 255) / 256 * 256); };
     if (p.c.rows) {
         p.rows_each = 16;

@@ -521,8 +521,8 @@ int hac_dot_noalloc(const hac_desc_t *desc, const void *d_blob,
 
 /* A chain of layers (not in the paper, which gives the product of one layer):
  *     A_0 = X,   A_{l+1} = act_l(A_l . W_l + bias_l),   Y = A_L
- * with W_l given compressed (HAC, sHAC, IM or MX; layer blobs of their own or the
- * layers of a network blob), bias_l an optional vector of m_l floats added to
+ * with W_l given compressed (HAC, sHAC, IM or MX; layer blobs of their own or, but
+ * for MX, the layers of a network blob), bias_l an optional vector of m_l floats added to
  * every row, act_l the identity or max(., 0).  Bias and activation are applied
  * where a sum is finished, and between two layers that both take the sparse
  * route the activations are written in the feature-major layout the next layer
@@ -611,8 +611,10 @@ int mx_decode_dev(const hac_desc_t *desc, const void *d_blob, uint32_t type, voi
 size_t mx_workspace_bytes(const hac_desc_t *desc, uint32_t type, int64_t B, uint32_t flags, int grouped);
 
 /* Y[B x m] = X[B x n] . W for a blob of one matrix.  Rows of X and Y may start at any element
- * (ldx >= n, ldy >= m); Y must not overlap X.  d_ws 256-byte aligned.  Results are bitwise reproducible:
- * sums are added in an order that the sizes alone determine. */
+ * (ldx >= n, ldy >= m); Y must not overlap X.  d_ws 256-byte aligned, of one call
+ * at a time.  Results are bitwise reproducible: sums are added in an order that the sizes alone
+ * determine.  More than 2^27 rows, and sizes whose blocks no launch can count (n or m of many
+ * millions), give HAC_ERANGE; other errors as for hac_dot. */
 int mx_dot(const hac_desc_t *desc, const void *d_blob, uint32_t type, const void *d_X, int64_t B, int64_t ldx,
            void *d_Y, int64_t ldy, uint32_t flags, void *d_ws, size_t ws_bytes, hac_stream_t stream);
 

@@ -1,5 +1,6 @@
 // Native call path of the Python binding for the calls of a serving loop: hac_dot, shac_dot, im_dot, hac_dot_noalloc,
-// hac_forward and the device calls of 4-bit layers (mx_*) on torch tensors.  Same checks, exceptions and results as the Python text they replace; nothing is kept
+// hac_forward and the device calls of 4-bit layers (mx_*) on torch tensors.  The first five have the checks, exceptions and
+// results of the Python text they replace; nothing is kept
 // between calls but the addresses of the library's functions.
 //
 // Why native: on small products the host, not the GPU, sets the time of a call.  A call through ctypes took 9 us of the

@@ -841,6 +841,7 @@ MxW matrices(const hac_desc_t& d, const void* blob)
 }
 
 constexpr int64_t kMostRows = 1 << 27;
+constexpr uint64_t kMostStretches = 65535;       // of 16 rows, in a launch of the kernel for few rows
 
 // How a product is split.  rows: the kernel for few rows, nc tiles of columns a block of `waves` wavefronts; else tiles of 16 nr rows x 64 nc
 // columns.  splits: parts that the k of a column are cut into.
@@ -899,7 +900,8 @@ Choice choose(const MxShape& s, uint64_t B, uint64_t count, uint64_t n, uint64_t
     auto consider = [&](double us, const Choice& c) { if (us < best_us) { best_us = us; best = c; } };
     const double stretches16 = live(16), x_mb = b * (double)n * (type == HAC_TYPE_F32 ? 4 : 2) / 1e6;
     const double step = k.steps + k.big * std::min(1.0, std::max(0.0, x_mb / 8 - 0.5)) + (type == HAC_TYPE_BF16 && n % 2 ? k.odd : 0.0);
-    for (uint32_t nc = 1; nc <= 4; nc *= 2) {
+    const bool rows_fit = fill(B, count, 16) <= kMostStretches;
+    for (uint32_t nc = 1; rows_fit && nc <= 4; nc *= 2) {
         const double blocks = stretches16 * (double)ceil_div(s.ctiles, nc), steps = blocks * (double)s.steps / 1024;
         for (uint32_t splits = 1; splits <= 16; splits *= 2) {
             if (splits > 1 && s.steps < 8 * splits) break;
@@ -918,7 +920,7 @@ Choice choose(const MxShape& s, uint64_t B, uint64_t count, uint64_t n, uint64_t
     const double laid = direct ? 0.0 : k.t_lay + k.t_lay_mb * b * (double)s.steps * 128 * (type == HAC_TYPE_F32 ? 4 : 2) / 1e6;
     const double w_mb = (count > 1 ? used : 1.0) * (double)n * (double)m / 2e6;
     const double fixed = k.t_call + laid + k.t_mb * out_mb * (type == HAC_TYPE_F32 ? 4 : 2) + k.t_w_mb * w_mb;
-    if (fixed >= best_us || B <= 8 * std::min(count, B)) return best;      // (up to 8 rows a group tiles were never measured to be quicker)
+    if (fixed >= best_us || (rows_fit && B <= 8 * std::min(count, B))) return best;      // (up to 8 rows a group tiles were never measured to be quicker)
     const uint32_t most_nr = mode == THREE ? 4 : 8;
     for (uint32_t nr = 2; nr <= most_nr; nr *= 2) {
         if (nr > 2 && B <= 8 * nr) break;
@@ -1065,7 +1067,7 @@ int run_typed(const Plan& p, const MxW& w, const void* X, uint64_t ldx, uint32_t
 bool grids_fit(const Plan& p, const MxShape& s, const hac_desc_t& d)
 {
     if (p.c.splits > 1 && ceil_div(d.m, 256) > 0xffffffull) return false;                 // (of the pass that adds them)
-    if (p.c.rows) return p.col_blocks <= 0xffffffffull / (64 * p.c.waves) && p.stretches <= 65535;
+    if (p.c.rows) return p.col_blocks <= 0xffffffffull / (64 * p.c.waves) && p.stretches <= kMostStretches;
     return p.tiles <= 0xffffffull && s.groups <= 65535 && p.stretches * p.col_blocks <= 0xfffff0ull / p.c.splits;
 }
 

@@ -318,6 +318,21 @@ def test_offsets_that_make_no_sense_stay_inside(hac):
                 assert bool((y[0] == 3).all()) and bool((y[-1] == 3).all())
 
 
+@pytest.mark.parametrize("both", [False, True])
+def test_a_million_rows(hac, both):
+    """More than 65535 stretches of 16 rows; the same rows in smaller calls, within both bounds."""
+    B, n, m = 65535 * 16 + 40, 40, 12
+    w = layer(n, m)
+    X = batch(1000, n, BF16).to(DEV).repeat(B // 1000 + 1, 1)[:B]
+    db = hac.mx_encode_dev(torch.from_numpy(w).to(DEV))
+    print(f"[case] {B} rows both={both}", flush=True)
+    Y = hac.mx_dot(db, X, quantize=both)
+    for at in (slice(0, 300), slice(B // 2, B // 2 + 300), slice(B - 300, B)):
+        check(Y[at], X[at].cpu(), w, both, at)
+    off = torch.tensor([0, B], dtype=torch.int32, device=DEV)
+    assert torch.equal(hac.mx_grouped_dot(db, X, off, quantize=both), Y)
+
+
 # ---- as they are used ----------------------------------------------------------------------------------
 
 

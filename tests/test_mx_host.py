@@ -250,3 +250,24 @@ def test_reads_of_a_step_that_is_not_whole_stay_inside_the_row(tmp_path):
     subprocess.run([gxx, "-std=c++17", "-O1", "-o", exe, os.path.join(ROOT, "tests", "native", "mx_reads.cpp")], check=True, timeout=120)
     run = subprocess.run([exe], capture_output=True, text=True, timeout=120)
     assert run.returncode == 0 and " 0 failures" in run.stdout, run.stdout
+
+
+# more rows than the kernel for few rows can count in a launch, whatever the layer
+MANY_ROWS = """
+out = []
+for n, m, count in ((1, 1, 1), (64, 10, 1), (4096, 64, 1), (64, 10, 3), (64, 10, 65535)):
+    d = hac.mx_describe(n, m, count)
+    for B in (300000, 65535 * 16, 65535 * 16 + 1, 1 << 24, 1 << 27):
+        for type in (0, 1):
+            for flags in (0, 1):
+                need = lib.mx_workspace_bytes(C.byref(d), type, B, flags, 1)
+                at = lambda x: C.c_void_p(x << 48)
+                stub.stub_reset()
+                out.append([n, m, count, B, lib.mx_grouped_dot(C.byref(d), at(1), type, at(2), B, n, at(3), at(4), m, flags, at(5), need, None), len(events())])
+print(json.dumps(out))
+"""
+
+
+def test_plans_of_many_rows(tmp_path):
+    for case in hip_stub.run(tmp_path, MANY_ROWS):
+        assert case[-2] == 0 and case[-1] >= 1, case

@@ -326,6 +326,16 @@ template <typename T> __device__ __forceinline__ void store4(T* y, uint32_t col,
         if (col + i < m) y[col + i] = (T)v[i];
 }
 
+// eight, of which `left` are inside the row, as bfloat16
+__device__ __forceinline__ void store8(__bf16* y, uint32_t left, u32x4 v)
+{
+    if (left >= 8) *reinterpret_cast<u32x4*>(y) = v;
+    else
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if ((uint32_t)i < left) reinterpret_cast<uint16_t*>(y)[i] = (uint16_t)(v[i / 2] >> 16 * (i & 1));
+}
+
 // ---- quantisation and its inverse ------------------------------------------------------------
 // A thread has a block: 32 rows of one column, so that the 64 lanes of a wavefront read 64 neighbouring columns row by row and need
 // no exchange.  A block of threads covers 64 columns x 512 rows, a group of scales: their bytes meet in LDS.  Bound by memory.
@@ -774,8 +784,30 @@ mx_tile_kernel(MxW w, const uint8_t* __restrict__ xt, const uint8_t* __restrict_
         else if (NR >= 4 && tiles <= NR * 3 / 4) walk(std::integral_constant<int, NR >= 4 ? NR * 3 / 4 : NR>{});
         else walk(std::integral_constant<int, NR>{});
     }
-    const uint32_t l16 = lane & 15, col0 = (cb * 4 + wave) * NC * 16 + 4 * (lane >> 4);
+    const uint32_t l16 = lane & 15, first_col = (cb * 4 + wave) * NC * 16, col0 = first_col + 4 * (lane >> 4);
     const bool wide = (reinterpret_cast<uintptr_t>(Y) | ldy * sizeof(T)) % (4 * sizeof(T)) == 0;
+    if constexpr (sizeof(T) == 2 && NC > 1) {
+        // two tiles of columns at a time: the lanes of a row exchange halves and have eight neighbouring columns each, so that an instruction
+        // writes 64 bytes of a row side by side, not 32 (4096 x 8192 results of k = 8192 in 4 bits 160 -> 156 us; 128 bytes: no better)
+        if (splits == 1 && (reinterpret_cast<uintptr_t>(Y) | ldy * 2) % 16 == 0) {
+#pragma unroll
+            for (int r = 0; r < NR; ++r)
+#pragma unroll
+                for (int q = 0; q < NC; q += 2) {
+                    uint32_t h[2][2];
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const f32x4 v = acc[r][q + i];
+                        h[i][0] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)v.x, (__bf16)v.y});
+                        h[i][1] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)v.z, (__bf16)v.w});
+                    }
+                    swap16(h[0][0], h[1][0]); swap16(h[0][1], h[1][1]);
+                    const uint32_t at = 16 * r + l16, col = first_col + 16 * (q + (lane >> 4 & 1)) + 8 * (lane >> 5);
+                    if (at < it.rows && col < w.m) store8(Y + (uint64_t)(it.row0 + at) * ldy + col, w.m - col, u32x4{h[0][0], h[0][1], h[1][0], h[1][1]});
+                }
+            return;
+        }
+    }
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
         const uint32_t at = 16 * r + l16;

@@ -318,6 +318,21 @@ def test_offsets_that_make_no_sense_stay_inside(hac):
                 assert bool((y[0] == 3).all()) and bool((y[-1] == 3).all())
 
 
+@pytest.mark.parametrize("m", [1496, 1500, 1501])
+@pytest.mark.parametrize("both", [False, True])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_rows_of_results_that_are_padded(hac, m, both, dtype):
+    """Rows of Y start at 16 bytes, their last entries do not fill them; what lies between two rows stays."""
+    B, n = 1030, 1024
+    w, X = layer(n, m), batch(B, n, dtype)
+    y = torch.full((B, 1504), 5.0, dtype=dtype, device=DEV)
+    print(f"[case] padded {dtype} m={m} both={both}", flush=True)
+    hac.mx_dot(hac.mx_encode_dev(torch.from_numpy(w).to(DEV)), X.to(DEV), y[:, :m], quantize=both)
+    assert "mx_tile_kernel" in hac.hac_last_kernels()
+    check(y[:, :m], X, w, both, m)
+    assert bool((y[:, m:] == 5).all())
+
+
 @pytest.mark.parametrize("both", [False, True])
 def test_a_million_rows(hac, both):
     """More than 65535 stretches of 16 rows; the same rows in smaller calls, within both bounds."""

@@ -137,7 +137,8 @@ template <> struct Block32<float> {
             for (int e = 0; e < 4; ++e) { uint32_t a = p[i][e], b = p[i + 2][e]; swap16(a, b); p[i][e] = a; p[i + 2][e] = b; }
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = __builtin_bit_cast(f32x4, p[(i & 2) << 1 | (i & 1) << 1 | i >> 2]);   // (register 4 p1 + 2 p0 + p2 has piece 8 g + 4 p2 + 2 p1 + p0)
+        for (int i = 0; i < 8; ++i) v[i] = __builtin_bit_cast(f32x4, p[(i & 2) << 1 | (i & 1) << 1 | i >> 2]);
+        // (register 4 p1 + 2 p0 + p2 has piece 8 g + 4 p2 + 2 p1 + p0)
     }
     __device__ __forceinline__ uint32_t most() const                             // bits of the largest magnitude
     {
@@ -338,7 +339,9 @@ __device__ __forceinline__ void store8(__bf16* y, uint32_t left, u32x4 v)
 
 // ---- quantisation and its inverse ------------------------------------------------------------
 // A thread has a block: 32 rows of one column, so that the 64 lanes of a wavefront read 64 neighbouring columns row by row and need
-// no exchange.  A block of threads covers 64 columns x 512 rows, a group of scales: their bytes meet in LDS.  Bound by memory.
+// no exchange.  A block of threads covers 64 columns x 512 rows, a group of scales: their bytes meet in LDS.  Bound by memory: 25088 x 4096
+// of fp32 are encoded in 127 us (466 MB moved, 3.7 TB/s) and decoded in 71 (6.6, the codes come from the last-level cache); a copy of
+// 1 GiB reaches 5.1.
 constexpr uint32_t kCodeCols = 64, kCodeRows = 512;
 
 template <typename T>
@@ -415,6 +418,9 @@ mx_decode_kernel(T* __restrict__ W, uint64_t ldw, uint64_t stride, MxW w)
 // columns (and, with splits, a range of k), its wavefronts share the steps, each reads its tiles of W straight into operands; X comes from memory
 // (from the L2 after the first block), is turned into parts or quantised by the lane that holds the block, and the wavefronts' sums are
 // added in LDS in order.  A lane past the last row reads that row again: what it adds goes to sums that nobody stores.
+// Bound by the launch and the first trips to memory where there is little work (4096 x 4096, one row of bfloat16: 4.8 us, the 8.9 MB of W alone
+// 1.8; 64 experts of 2048 x 1408, 64 rows: 13, the W of those that have rows 8.6), by the turning of X into operands, which every block of columns
+// repeats, where there is more: from some hundreds of rows on tiles are quicker, and the estimates below say which.
 template <int MODE, typename T, int NC, int U>
 __global__ void __launch_bounds__(512)
 mx_rows_kernel(MxW w, const T* __restrict__ X, uint64_t ldx, uint32_t B, const int32_t* __restrict__ offsets,
@@ -513,7 +519,7 @@ mx_rows_kernel(MxW w, const T* __restrict__ X, uint64_t ldx, uint32_t B, const i
 // X in operand order, group by group, each group from a tile of 16 rows of its own on, zeros behind entry n up to a whole group of four steps: quantised codes (and
 // their scales in groups of four tiles, as W's); bf16 rows as [tile][step][row][piece of 8 k], pieces in an order that differs from
 // row to row (turned); the three parts of fp32 rows as [tile][step][half][part][operand][lane][16 bytes].
-// (A wavefront has a tile's step, a lane a block of its row.)
+// (A wavefront has a tile's step, a lane a block of its row.)  Bound by memory: 4096 rows of 8192 bfloat16 to codes in 20 us, 4.1 TB/s.
 __host__ __device__ constexpr uint32_t step_bytes(int mode) { return mode == FP4 ? 1024u : 4096u * mode; }
 // Steps of a chunk, which is what a block stages and requests at once, and chunks of a step.  Few rows are multiplied quickly: several steps
 // at once keep more of W in flight (9973 x 1511, 137 bf16 rows 24.0 -> 20.8 us), unless three parts of them leave LDS room for one block
@@ -572,6 +578,9 @@ mx_lay_out_kernel(const T* __restrict__ X, uint64_t ldx, uint32_t n, uint32_t gr
 // The order of a chunk is spelled out in beats of NC matrix instructions: left to itself the compiler reads an operand right before its
 // use and waits.  A beat's operand of X is read two beats ahead, and W's operands of the next 32 k are expanded beside this one's products.
 // DIRECT: bf16 rows whose pieces of 8 k are whole and aligned need no laying out, they are staged from where they are.
+// Measured: 4096 x 4096, 2048 rows of bfloat16 60 us, 1.15 PFLOP/s, 8 groups of it with 4096 rows 1.0 (a library's bfloat16 product of the first size
+// 1.01, of 8192 x 8192 x 8192 1.26; the instructions alone, from registers, 1.8); 8192 x 8192, 4096 rows in codes 138 us, 4.0 PFLOP/s (7.1 from
+// registers; without W's loads 24 us less, without staging 20, without either 45).
 __device__ __constant__ __attribute__((aligned(16))) uint32_t zeros16[4] = {0, 0, 0, 0};
 
 // 16 bytes (4) a lane from memory to lds + 16 (4) * lane, past the registers.  In assembly, so that the compiler counts its own loads only: with
@@ -824,7 +833,7 @@ mx_tile_kernel(MxW w, const uint8_t* __restrict__ xt, const uint8_t* __restrict_
 }
 
 // Y = part[0] + part[1] + ... in that order, for the rows that some group holds.  A thread has four neighbouring sums where columns come in fours
-// (V = f32x4), so that all splits' are in flight.
+// (V = f32x4), so that all splits' are in flight.  16 splits of 32 x 4096 sums: 3.9 us, of which 2 are the launch.
 template <typename T, typename V>
 __global__ void __launch_bounds__(256)
 mx_sum_kernel(const float* __restrict__ part, uint32_t splits, uint32_t B, uint32_t m, const int32_t* __restrict__ offsets, uint32_t count,
@@ -879,6 +888,7 @@ constexpr uint64_t kMostStretches = 65535;       // of 16 rows, in a launch of t
 // columns.  splits: parts that the k of a column are cut into.
 struct Choice { bool rows; uint32_t nr, nc, waves, splits; };
 
+constexpr uint32_t least_nc(int mode, uint32_t nr) { return mode == THREE || nr == 8 ? 2 : 1; }           // (one column tile was never the quickest there)
 constexpr uint32_t most_nc(int mode, uint32_t nr) { return mode == ONE && nr == 8 ? 2 : 4; }       // (more sums and operands than registers)
 
 struct Plan {
@@ -895,27 +905,28 @@ uint64_t fill(uint64_t B, uint64_t count, uint64_t R) { return std::min<uint64_t
 
 // The split with the shortest estimate of a call's time.  Its form and constants (us) were fitted to the measured times of all splits of 800 products
 // drawn over n 64 .. 25088, m 10 .. 8192, 1 .. 12544 rows, 1 .. 64 groups: estimates are off by 10 to 14 % in the mean, and the splits they choose are
-// 3.0 % slower in the mean than the best measured ones, at most 1.47 times (one split per kernel, chosen by rows alone: 45 %).
+// 3.0 % slower in the mean than the best measured ones, at most 1.47 times, and 3.7 % over 350 products that they were not fitted to (one split per
+// kernel, chosen by rows alone: 45 %).
 //   few rows: a launch; trips to memory, two steps each, and what a trip grows by with each tile of columns; wavefronts beyond eight on a CU;
 //     steps of X turned into operands and of W multiplied per SIMD, what the former cost more where X is larger than the L2s (big) or its rows of
 //     bfloat16 have an odd length, and those that a SIMD has more where blocks are fewer than CUs; sums stored; the pass that adds the
 //     splits and its megabytes
 //   tiles: a launch; X laid out and its megabytes; chunks of a block and their matrix instructions; the blocks of a CU; a hundred steps of a
-//     block times the blocks of a CU, for 2, 4, 8 tiles of rows and 1, 2, 4 of columns a wavefront; the pass that adds the splits and its
-//     megabytes; Y's megabytes and W's
+//     block times the blocks of a CU, for 2, 4, 8 tiles of rows and 1, 2, 4 of columns a wavefront (0: there is no such kernel); the pass that adds the
+//     splits and its megabytes; Y's megabytes and W's
 struct Costs {
     double call, trip, trip_nc, waves, steps, steps_nc, big, odd, alone, sums, split, split_mb;
     double t_call, t_lay, t_lay_mb, t_chunk, t_chunk_mm, t_cu, t_tile[9], t_split, t_split_mb, t_mb, t_w_mb;
 };
 const Costs kCosts[4] = {
     { 3.85, 0.456, 0.074, 0.414, 0.584, 0.081, 0.360, 0.000, 0.311, 0.435, 1.92, 4.51,                      // codes, from fp32
-      0.00, 7.60, 0.199, 0.014, 0.029, 0.000, { 6.58, 10.7, 20.4, 11.4, 16.7, 28.8, 23.0, 30.5, 58.9 }, 1.77, 2.23, 0.583, 0.122 },
+      0.00, 7.60, 0.199, 0.014, 0.029, 0.000, { 6.58, 10.7, 20.4, 11.4, 16.7, 28.8, 0.0, 30.5, 58.9 }, 1.77, 2.23, 0.583, 0.122 },
     { 3.64, 0.609, 0.082, 0.354, 0.203, 0.070, 0.269, 0.222, 0.219, 0.381, 2.19, 2.93,                      // codes, from bf16
-      0.00, 7.13, 0.246, 0.012, 0.790, 0.000, { 5.48, 8.69, 15.4, 8.84, 11.9, 17.6, 17.7, 19.2, 29.6 }, 2.63, 1.65, 0.780, 0.082 },
+      0.00, 7.13, 0.246, 0.012, 0.790, 0.000, { 5.48, 8.69, 15.4, 8.84, 11.9, 17.6, 0.0, 19.2, 29.6 }, 2.63, 1.65, 0.780, 0.082 },
     { 3.39, 0.845, 0.270, 0.793, 0.597, 0.121, 0.474, 0.000, 0.335, 0.387, 2.63, 1.73,                      // fp32
-      0.00, 8.16, 0.557, 0.249, 0.329, 0.000, { 44.8, 61.6, 84.9, 91.6, 113.0, 176.0 }, 2.11, 1.60, 0.658, 0.000 },
+      0.00, 8.16, 0.557, 0.249, 0.329, 0.000, { 0.0, 61.6, 84.9, 0.0, 113.0, 176.0 }, 2.11, 1.60, 0.658, 0.000 },
     { 3.66, 0.493, 0.159, 0.392, 0.031, 0.087, 0.280, 0.424, 0.145, 0.285, 2.18, 2.77,                      // bf16
-      3.72, 3.60, 0.648, 0.196, 0.465, 0.356, { 15.8, 21.6, 36.9, 29.4, 37.8, 55.3, 54.6, 67.0 }, 2.28, 1.87, 0.957, 0.001 },
+      3.72, 3.60, 0.648, 0.196, 0.465, 0.356, { 15.8, 21.6, 36.9, 29.4, 37.8, 55.3, 0.0, 67.0 }, 2.28, 1.87, 0.957, 0.001 },
 };
 
 Choice choose(const MxShape& s, uint64_t B, uint64_t count, uint64_t n, uint64_t m, uint32_t type, int mode, bool direct)
@@ -960,7 +971,7 @@ Choice choose(const MxShape& s, uint64_t B, uint64_t count, uint64_t n, uint64_t
         if (count == 1) { const uint64_t tiles = ceil_div(B, 16); rows = 16 * ceil_div(tiles, ceil_div(tiles, nr)); }   // (dealt evenly)
         const uint64_t chunks = ceil_div(s.steps, chunk_steps(mode, nr));
         const double stretches = live(rows);
-        for (uint32_t nc = 1; nc <= most_nc(mode, nr); nc *= 2) {
+        for (uint32_t nc = least_nc(mode, nr); nc <= most_nc(mode, nr); nc *= 2) {
             const double blocks = stretches * (double)ceil_div(s.ctiles, 4 * nc);
             const double step_us = k.t_tile[(nr / 4) * 3 + nc / 2] / 100 * chunk_steps(mode, nr) * (0.2 + 0.8 * (double)rows / (16 * nr));
             const double mm = (mode == FP4 ? 1.0 : mode == THREE ? 4.0 * 3 : 4.0) * chunk_steps(mode, nr) * (double)(rows / 16) * nc / 100;
@@ -1014,7 +1025,8 @@ int launch_rows(const Plan& p, const MxW& w, const T* X, uint64_t ldx, uint32_t 
 {
     constexpr int U = 2;
     hipLaunchKernelGGL((mx_rows_kernel<MODE, T, NC, U>), dim3((uint32_t)p.col_blocks, (uint32_t)p.stretches, p.c.splits), dim3(64 * p.c.waves),
-                       (size_t)p.c.waves * NC * 1024, stream, w, X, ldx, B, offsets, Y, ldy, w.steps / (p.c.splits * p.c.waves), w.steps % (p.c.splits * p.c.waves), part);
+                       (size_t)p.c.waves * NC * 1024, stream, w, X, ldx, B, offsets, Y, ldy, w.steps / (p.c.splits * p.c.waves),
+                       w.steps % (p.c.splits * p.c.waves), part);
     note_kernel("mx_rows_kernel<%d, %s, %d, %d>", MODE, type_name(X), NC, U);
     return launched();
 }
@@ -1046,7 +1058,8 @@ int pick_tile(const Plan& p, const MxW& w, const Operands& x, uint32_t B, const 
 {
     auto columns = [&](auto rows) {
         constexpr int NR = decltype(rows)::value;
-        if (p.c.nc == 1) return launch_tile<MODE, DIRECT, T, NR, 1>(p, w, x, B, offsets, Y, ldy, stream);
+        if constexpr (least_nc(MODE, NR) == 1)
+            if (p.c.nc == 1) return launch_tile<MODE, DIRECT, T, NR, 1>(p, w, x, B, offsets, Y, ldy, stream);
         if constexpr (most_nc(MODE, NR) == 4)
             if (p.c.nc == 4) return launch_tile<MODE, DIRECT, T, NR, 4>(p, w, x, B, offsets, Y, ldy, stream);
         return launch_tile<MODE, DIRECT, T, NR, 2>(p, w, x, B, offsets, Y, ldy, stream);

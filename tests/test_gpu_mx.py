@@ -348,6 +348,46 @@ def test_a_million_rows(hac, both):
     assert torch.equal(hac.mx_grouped_dot(db, X, off, quantize=both), Y)
 
 
+def test_results_past_32_bits(hac):
+    """4.9 GB of results: the last rows are what the same rows give alone, within both bounds."""
+    B, n, m = 300000, 32, 8192
+    w = layer(n, m)
+    X = batch(1000, n, BF16).to(DEV).repeat(B // 1000, 1)
+    db = hac.mx_encode_dev(torch.from_numpy(w).to(DEV))
+    print("[case] 300000 x 8192 results", flush=True)
+    Y = hac.mx_dot(db, X)
+    for at in (slice(0, 40), slice(B - 40, B)):
+        check(Y[at], X[at].cpu(), w, False, at)
+    assert torch.equal(Y[1000:1040], Y[B - 1000:B - 960])
+
+
+def test_a_blob_past_32_bits(hac):
+    """520 matrices of 4096 x 4096, 4.6 GB of codes: encoded, decoded and multiplied where offsets do not fit 32 bits."""
+    count, n = 520, 4096
+    g = torch.Generator(device=DEV)
+    g.manual_seed(1)
+    W = torch.empty((count, n, n), dtype=BF16, device=DEV)
+    W[:2].normal_(generator=g)
+    W[2:] = 0
+    W[-1].normal_(generator=g)
+    print("[case] 520 matrices of 4096 x 4096", flush=True)
+    db = hac.mx_encode_dev(W)
+    alone = [hac.mx_encode_dev(W[e]) for e in (0, count - 1)]
+    back = hac.mx_decode_dev(db, BF16)
+    for e, one in zip((0, count - 1), alone):
+        assert torch.equal(back[e], hac.mx_decode_dev(one, BF16))
+    assert not bool(back[2:-1].any())
+    del back, W
+    for rows in (5, 300):
+        for both in (False, True):
+            X = batch(2 * rows, n, BF16).to(DEV)
+            off = torch.full((count + 1,), rows, dtype=torch.int32, device=DEV)
+            off[0], off[-1] = 0, 2 * rows
+            Y = hac.mx_grouped_dot(db, X, off, quantize=both)
+            for e, one, at in zip((0, count - 1), alone, (slice(0, rows), slice(rows, 2 * rows))):
+                check(Y[at], X[at].cpu(), hac.mx_decode_dev(one).cpu().numpy(), both, (e, rows))
+
+
 # ---- as they are used ----------------------------------------------------------------------------------
 
 

@@ -339,12 +339,14 @@ __device__ __forceinline__ void store8(__bf16* y, uint32_t left, u32x4 v)
 
 // ---- quantisation and its inverse ------------------------------------------------------------
 // A thread has a block: 32 rows of one column, so that the 64 lanes of a wavefront read 64 neighbouring columns row by row and need
-// no exchange.  A block of threads covers 64 columns x 512 rows, a group of scales: their bytes meet in LDS.  Bound by memory: 25088 x 4096
-// of fp32 are encoded in 127 us (466 MB moved, 3.7 TB/s) and decoded in 71 (6.6, the codes come from the last-level cache); a copy of
-// 1 GiB reaches 5.1.
+// no exchange.  A block of threads covers 64 columns x 512 rows, a group of scales: their bytes meet in LDS.  Bound by memory.
+// STREAM: past the last-level cache, for W larger than that.  25088 x 4096 of fp32 (411 MB) to codes and back 197 us, with streamed loads 167, with streamed
+// stores 175; 16 x 1024 x 2048 of bfloat16 (67 MB) 30, 34.6 and 29, and whoever reads the values next finds them in the cache without.
+// (Two columns a thread: 230 and 34.)
+constexpr uint64_t kCacheBytes = 256ull << 20;
 constexpr uint32_t kCodeCols = 64, kCodeRows = 512;
 
-template <typename T>
+template <typename T, bool STREAM>
 __global__ void __launch_bounds__(1024)
 mx_encode_kernel(const T* __restrict__ W, uint64_t ldw, uint64_t stride, MxW w, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales,
                  uint8_t* __restrict__ header, hac_desc_t desc)
@@ -360,7 +362,7 @@ mx_encode_kernel(const T* __restrict__ W, uint64_t ldw, uint64_t stride, MxW w, 
     const T* p = W + e * stride + (uint64_t)k * ldw + j;
     if (j < w.m && k + 32 <= w.n) {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) x.v[i / 4][i % 4] = (float)p[(uint64_t)i * ldw];
+        for (int i = 0; i < 32; ++i) x.v[i / 4][i % 4] = (float)(STREAM ? __builtin_nontemporal_load(p + (uint64_t)i * ldw) : p[(uint64_t)i * ldw]);
     } else {
 #pragma unroll
         for (int i = 0; i < 32; ++i) x.v[i / 4][i % 4] = j < w.m && k + i < w.n ? (float)p[(uint64_t)i * ldw] : 0.0f;
@@ -381,7 +383,7 @@ mx_encode_kernel(const T* __restrict__ W, uint64_t ldw, uint64_t stride, MxW w, 
     }
 }
 
-template <typename T>
+template <typename T, bool STREAM>
 __global__ void __launch_bounds__(1024)
 mx_decode_kernel(T* __restrict__ W, uint64_t ldw, uint64_t stride, MxW w)
 {
@@ -410,7 +412,11 @@ mx_decode_kernel(T* __restrict__ W, uint64_t ldw, uint64_t stride, MxW w)
     const uint32_t rows = min(32u, w.n - k);
 #pragma unroll
     for (int i = 0; i < 32; ++i)
-        if ((uint32_t)i < rows) p[(uint64_t)i * ldw] = (T)(byte == 255 ? __builtin_nanf("") : v[i]);
+        if ((uint32_t)i < rows) {
+            const T value = (T)(byte == 255 ? __builtin_nanf("") : v[i]);
+            if constexpr (STREAM) __builtin_nontemporal_store(value, p + (uint64_t)i * ldw);
+            else p[(uint64_t)i * ldw] = value;
+        }
 }
 
 // ---- few rows, or little work ------------------------------------------------------------------
@@ -1150,6 +1156,14 @@ bool code_grid(const hac_desc_t& d, dim3& grid)
     return true;
 }
 
+// calls launch(an element of W, whether W is streamed)
+template <typename F> void by_size(const hac_desc_t& d, uint32_t type, F launch)
+{
+    const bool large = (uint64_t)d.k_sym * d.n * d.m * (type == HAC_TYPE_F32 ? 4 : 2) > kCacheBytes;
+    if (type == HAC_TYPE_F32) { if (large) launch(0.0f, std::true_type{}); else launch(0.0f, std::false_type{}); }
+    else { if (large) launch((__bf16)0.0f, std::true_type{}); else launch((__bf16)0.0f, std::false_type{}); }
+}
+
 bool layout_ok(const hac_desc_t& d, int64_t ldw, int64_t stride)
 {
     return ldw >= (int64_t)d.m && (d.k_sym == 1 || (stride >= 0 && stride / ldw >= (int64_t)d.n));
@@ -1184,13 +1198,14 @@ extern "C" int mx_encode_dev(uint32_t type, const void* d_W, int64_t count, int6
     uint8_t* b = static_cast<uint8_t*>(d_blob);
     hipStream_t hs = static_cast<hipStream_t>(stream);
     const uint64_t apart = count > 1 ? (uint64_t)stride : 0;
-    if (type == HAC_TYPE_F32)
-        hipLaunchKernelGGL(mx_encode_kernel<float>, grid, dim3(1024), 0, hs, static_cast<const float*>(d_W), (uint64_t)ldw, apart, w,
-                           b + d.off_stream, b + d.off_codebook, b, d);
-    else
-        hipLaunchKernelGGL(mx_encode_kernel<__bf16>, grid, dim3(1024), 0, hs, static_cast<const __bf16*>(d_W), (uint64_t)ldw, apart, w,
-                           b + d.off_stream, b + d.off_codebook, b, d);
-    note_kernel("mx_encode_kernel<%s>", type == HAC_TYPE_F32 ? "float" : "__bf16");
+    auto launch = [&](auto element, auto stream_it) {
+        using T = decltype(element);
+        constexpr bool S = decltype(stream_it)::value;
+        hipLaunchKernelGGL((mx_encode_kernel<T, S>), grid, dim3(1024), 0, hs, static_cast<const T*>(d_W), (uint64_t)ldw, apart, w, b + d.off_stream,
+                           b + d.off_codebook, b, d);
+        note_kernel("mx_encode_kernel<%s, %s>", type_name(static_cast<const T*>(d_W)), S ? "true" : "false");
+    };
+    by_size(d, type, launch);
     return launched();
 }
 
@@ -1206,9 +1221,13 @@ extern "C" int mx_decode_dev(const hac_desc_t* desc, const void* d_blob, uint32_
     const MxW w = matrices(*desc, d_blob);
     hipStream_t hs = static_cast<hipStream_t>(stream);
     const uint64_t apart = desc->k_sym > 1 ? (uint64_t)stride : 0;
-    if (type == HAC_TYPE_F32) hipLaunchKernelGGL(mx_decode_kernel<float>, grid, dim3(1024), 0, hs, static_cast<float*>(d_W), (uint64_t)ldw, apart, w);
-    else hipLaunchKernelGGL(mx_decode_kernel<__bf16>, grid, dim3(1024), 0, hs, static_cast<__bf16*>(d_W), (uint64_t)ldw, apart, w);
-    note_kernel("mx_decode_kernel<%s>", type == HAC_TYPE_F32 ? "float" : "__bf16");
+    auto launch = [&](auto element, auto stream_it) {
+        using T = decltype(element);
+        constexpr bool S = decltype(stream_it)::value;
+        hipLaunchKernelGGL((mx_decode_kernel<T, S>), grid, dim3(1024), 0, hs, static_cast<T*>(d_W), (uint64_t)ldw, apart, w);
+        note_kernel("mx_decode_kernel<%s, %s>", type_name(static_cast<const T*>(d_W)), S ? "true" : "false");
+    };
+    by_size(*desc, type, launch);
     return launched();
 }
 

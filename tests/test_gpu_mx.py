@@ -361,6 +361,22 @@ def test_results_past_32_bits(hac):
     assert torch.equal(Y[1000:1040], Y[B - 1000:B - 960])
 
 
+@pytest.mark.parametrize("dtype,n", [(F32, 20001), (BF16, 40001)])
+def test_a_matrix_larger_than_the_cache(hac, dtype, n):
+    """Streamed past the last-level cache; its column halves, which are not, have the same bytes and values."""
+    m = 4100
+    g = torch.Generator(device=DEV)
+    g.manual_seed(2)
+    W = torch.randn((n, m), generator=g, device=DEV).to(dtype)
+    print(f"[case] {n} x {m} {dtype}", flush=True)
+    values = hac.mx_decode_dev(hac.mx_encode_dev(W), dtype)
+    assert hac.hac_last_kernels()[0].endswith("true>")
+    for part in (slice(0, 2048), slice(2048, m)):
+        half = hac.mx_decode_dev(hac.mx_encode_dev(W[:, part]), dtype)
+        assert hac.hac_last_kernels()[0].endswith("false>") and torch.equal(values[:, part], half)
+    assert np.array_equal(values[:700, -5:].double().cpu().numpy()[:672], mx.values(W[:700, -5:].float().cpu().numpy())[:672])
+
+
 def test_a_blob_past_32_bits(hac):
     """520 matrices of 4096 x 4096, 4.6 GB of codes: encoded, decoded and multiplied where offsets do not fit 32 bits."""
     count, n = 520, 4096

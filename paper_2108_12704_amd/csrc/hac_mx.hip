@@ -340,9 +340,9 @@ __device__ __forceinline__ void store8(__bf16* y, uint32_t left, u32x4 v)
 // ---- quantisation and its inverse ------------------------------------------------------------
 // A thread has a block: 32 rows of one column, so that the 64 lanes of a wavefront read 64 neighbouring columns row by row and need
 // no exchange.  A block of threads covers 64 columns x 512 rows, a group of scales: their bytes meet in LDS.  Bound by memory.
-// STREAM: past the last-level cache, for W larger than that.  25088 x 4096 of fp32 (411 MB) to codes and back 197 us, with streamed loads 167, with streamed
-// stores 175; 16 x 1024 x 2048 of bfloat16 (67 MB) 30, 34.6 and 29, and whoever reads the values next finds them in the cache without.
-// (Two columns a thread: 230 and 34.)
+// STREAM: past the last-level cache, for W larger than that.  25088 x 4096 of fp32 (411 MB) are encoded in 87 us (5.3 TB/s of a copy's 5.1) and decoded in
+// 80, not streamed in 98 and 93, one after the other in 168 and 197; 16 x 1024 x 2048 of bfloat16 (67 MB) one after the other in 35 with streamed
+// loads, 30 without, and whoever reads the values next finds them in the cache.  (Two columns a thread: 230 and 34.)
 constexpr uint64_t kCacheBytes = 256ull << 20;
 constexpr uint32_t kCodeCols = 64, kCodeRows = 512;
 

@@ -62,6 +62,10 @@ HAC_MX_BOTH inline bool mx_piece_at(uint32_t k, uint32_t left, uint32_t E, int32
     return left != 0;
 }
 
+// Whether those E entries (4: of fp32, 8: of bfloat16) begin at a word, in rows of which every one does (words: or not).  A row of bfloat16 of odd length
+// may have its last E begin inside one all the same.
+HAC_MX_BOTH inline bool mx_piece_words(int32_t at, uint32_t E, bool words) { return words && (E == 4 || at % 2 == 0); }
+
 // The header of `count` matrices of n x m; false where they are too many or too large.
 inline bool mx_header(int64_t count, int64_t n, int64_t m, hac_desc_t& d)
 {

@@ -61,7 +61,7 @@ __device__ __forceinline__ void swap16(uint32_t& a, uint32_t& b)
 // load_step: lane 16 g + c has row c and wants its entries 32 g ... of a step of 128.  Read that way, a load of 16 bytes a lane touches 64 lines; so
 // the four lanes of a row read 64 bytes side by side and then exchange pieces.
 // 16 bytes of a row from any entry on.  Loads that start at a word are as quick as aligned ones, loads that start inside a word several times
-// slower; so where rows of bfloat16 may (not `words`), the words that hold the entries are read and shifted.  A word that holds an entry is
+// slower; so where entries of bfloat16 may (not `words`), the words that hold them are read and shifted.  A word that holds an entry is
 // readable as a whole.
 template <typename T> __device__ __forceinline__ bool whole_words(const T* X, uint64_t ldx)      // every row begins at a word
 {
@@ -96,7 +96,7 @@ template <typename T> __device__ __forceinline__ u32x4 piece_of(const T* row, ui
     int32_t at;
     if (!mx_piece_at(k, left, E, at)) return p;
     const int d = (int)k - at;
-    p = load16(row + at, words);
+    p = load16(row + at, mx_piece_words(at, E, words));
     if constexpr (E == 8) {
         if (d & 1) p = u32x4{p.x >> 16 | p.y << 16, p.y >> 16 | p.z << 16, p.z >> 16 | p.w << 16, p.w >> 16};
     }

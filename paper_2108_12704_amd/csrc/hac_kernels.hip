@@ -955,10 +955,10 @@ thread_local int g_last_hip_error = 0;
 
 int hip_fail(hipError_t e) { g_last_hip_error = (int)e; return HAC_EHIP; }
 
-// What the planning calls need of a header before they divide by its fields (the device calls
-// check more, in make_dev and im_dot_impl).
 bool is_mx(const hac_desc_t* d) { return d && d->format == HAC_FORMAT_MX; }
 
+// What the planning calls need of a header of another format before they divide by its fields (the
+// device calls check more, in make_dev and im_dot_impl).
 bool desc_plausible(const hac_desc_t* d)
 {
     if (!d || d->magic != 0x31434148u || d->version != 2) return false;

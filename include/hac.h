@@ -577,8 +577,8 @@ int im_dot(const hac_desc_t *desc, const void *d_blob,
  * Codes and scales past row n or column m are 0.
  *
  * Values are X.W with W's entries so rounded: every value of W is exact in bfloat16 and sums are
- * kept in fp32.  X and Y are fp32 or bfloat16 (type; Y is rounded once, to nearest); fp32 rows of
- * X enter whole, as three bfloat16 parts, exactly but for what lies below 2^-133.  With
+ * kept in fp32, subnormal ones included.  X and Y are fp32 or bfloat16 (type; Y is rounded once, to
+ * nearest); fp32 rows of X enter whole, as three bfloat16 parts, exactly but for what lies below 2^-133.  With
  * HAC_MX_QUANTIZE_X the rows of X are quantised too, blocks of 32 entries of a row from its first
  * on, in the same way as columns of W: the product is then that of two matrices of 4-bit entries.
  * An infinity or NaN in X makes those results of its row NaN or infinite that the sum of its products
@@ -607,7 +607,9 @@ int mx_decode_dev(const hac_desc_t *desc, const void *d_blob, uint32_t type, voi
                   hac_stream_t stream);
 
 /* Device workspace of mx_dot for B rows, or of mx_grouped_dot for B rows in all (grouped != 0); 0
- * when none is needed and for arguments the calls refuse. */
+ * when none is needed and for arguments the calls refuse.  The size is the same wherever X lies and
+ * includes room for X in the order of the matrix units, which large products of bfloat16 rows that are
+ * whole, aligned pieces of 16 bytes leave unused. */
 size_t mx_workspace_bytes(const hac_desc_t *desc, uint32_t type, int64_t B, uint32_t flags, int grouped);
 
 /* Y[B x m] = X[B x n] . W for a blob of one matrix.  Rows of X and Y may start at any element

@@ -62,7 +62,7 @@ __device__ __forceinline__ void swap16(uint32_t& a, uint32_t& b)
 // the four lanes of a row read 64 bytes side by side and then exchange pieces.
 // 16 bytes of a row from any entry on.  Loads that start at a word are as quick as aligned ones, loads that start inside a word several times
 // slower; so where entries of bfloat16 may (not `words`), the words that hold them are read and shifted.  A word that holds an entry is
-// readable as a whole.
+// readable as a whole.  (301 x 400, 64 rows: 3.5 us with every second row inside a word, 3.1 with the ends of rows alone, 302 x 400 2.8.)
 template <typename T> __device__ __forceinline__ bool whole_words(const T* X, uint64_t ldx)      // every row begins at a word
 {
     return sizeof(T) == 4 || ((reinterpret_cast<uintptr_t>(X) | 2 * ldx) & 3) == 0;
@@ -585,8 +585,8 @@ mx_lay_out_kernel(const T* __restrict__ X, uint64_t ldx, uint32_t n, uint32_t gr
 // use and waits.  A beat's operand of X is read two beats ahead, and W's operands of the next 32 k are expanded beside this one's products.
 // DIRECT: bf16 rows whose pieces of 8 k are whole and aligned need no laying out, they are staged from where they are.
 // Measured: 4096 x 4096, 2048 rows of bfloat16 60 us, 1.15 PFLOP/s, 8 groups of it with 4096 rows 1.0 (a library's bfloat16 product of the first size
-// 1.01, of 8192 x 8192 x 8192 1.26; the instructions alone, from registers, 1.8); 8192 x 8192, 4096 rows in codes 138 us, 4.0 PFLOP/s (7.1 from
-// registers; without W's loads 24 us less, without staging 20, without either 45).
+// 1.01, of 8192 x 8192 x 8192 1.26; the instructions alone, from registers, 1.8); 8192 x 8192, 4096 rows in codes 137 us, 4.0 PFLOP/s (7.1 from
+// registers; without W's loads 24 us less, without staging 20, without either 45; 137 is the least of a trace, its median is 144, 3.8 PFLOP/s).
 __device__ __constant__ __attribute__((aligned(16))) uint32_t zeros16[4] = {0, 0, 0, 0};
 
 // 16 bytes (4) a lane from memory to lds + 16 (4) * lane, past the registers.  In assembly, so that the compiler counts its own loads only: with
@@ -912,7 +912,11 @@ uint64_t fill(uint64_t B, uint64_t count, uint64_t R) { return std::min<uint64_t
 // The split with the shortest estimate of a call's time.  Its form and constants (us) were fitted to the measured times of all splits of 800 products
 // drawn over n 64 .. 25088, m 10 .. 8192, 1 .. 12544 rows, 1 .. 64 groups: estimates are off by 10 to 14 % in the mean, and the splits they choose are
 // 3.0 % slower in the mean than the best measured ones, at most 1.47 times, and 3.7 % over 350 products that they were not fitted to (one split per
-// kernel, chosen by rows alone: 45 %).
+// kernel, chosen by rows alone: 45 %).  These figures are of the time of the fit: since then results in bfloat16 leave 64 bytes of a row side by side, which
+// takes 2 to 6 % off products on tiles.  The constants predict, they do not explain: on tiles quantised X is multiplied by the same loop whatever
+// its type was, yet the fit put that loop's time into t_tile for fp32 and into t_chunk_mm, in part, for bfloat16.  Too low where blocks are fewer than
+// CUs: 4096 x 4096, 16 quantised fp32 rows take 11.6 us in 64 blocks, estimated at 9.1; in four splits of four wavefronts they take 9.1.  Groups are taken
+// to be as full as a router leaves them: one in five or so without rows (used).
 //   few rows: a launch; trips to memory, two steps each, and what a trip grows by with each tile of columns; wavefronts beyond eight on a CU;
 //     steps of X turned into operands and of W multiplied per SIMD, what the former cost more where X is larger than the L2s (big) or its rows of
 //     bfloat16 have an odd length, and those that a SIMD has more where blocks are fewer than CUs; sums stored; the pass that adds the
@@ -994,7 +998,8 @@ Choice choose(const MxShape& s, uint64_t B, uint64_t count, uint64_t n, uint64_t
     return best;
 }
 
-// whole: rows of X consist of whole, aligned pieces of 16 bytes.  bytes is what a call needs wherever X lies.
+// whole: rows of X consist of whole, aligned pieces of 16 bytes.  bytes is what a call needs wherever X lies, for its size is asked without X: where
+// tiles take X as it lies, xt_bytes of it stay unused.
 Plan plan_mx(const hac_desc_t& d, uint32_t type, uint64_t B, uint32_t flags, bool grouped, bool whole)
 {
     const MxShape s = mx_shape(d.n, d.m);
